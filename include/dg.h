@@ -19,6 +19,11 @@
  *   dg_assemble_batch  feature assembling (§4, Fig. 3): merge cache rows and packed
  *                      rows into one mini-batch's input tensor, in sampled order.
  *
+ * Further calls work on the rows that a model computes from a mini-batch (paper §2,
+ * Eq. 1): rows of a learned embedding table and their gradient, an RMS norm with an
+ * 8-bit output, and attention of the frontier nodes over their sampled neighbours, each
+ * with its gradient (see "Model rows" below).
+ *
  * Everything lives in device memory (HBM): the disk tiers of the paper are not
  * part of this library.
  *
@@ -564,6 +569,143 @@ size_t dg_minhash_workspace_bytes(int64_t m);
 int dg_minhash_order(const uint64_t *membership, int64_t N, int32_t B, const int32_t *entries,
                      int64_t m, const int32_t *perms, int32_t k, int32_t *order,
                      int32_t *signature, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------------
+ * Model rows
+ * ------------------------------------------------------------------------------
+ * Elements are of a dg_dtype; sums, norms and softmax statistics are computed in 32
+ * bits, and a result is rounded (to nearest, ties to even) once, when it is stored.
+ * Strides are in elements, between the first elements of consecutive rows; a row's own
+ * elements are adjacent.  No pointer needs more alignment than its elements.  All calls
+ * are asynchronous on `stream`; those with a workspace (256-aligned) use it until that
+ * work is done.  Results do not depend on the order in which blocks run: the same
+ * inputs give the same bits.  Optional `status`: a device int32 into which the kernels
+ * OR 1 for an index out of range and 2 for offsets or edges out of order; what such an
+ * entry adds is left out, and no access falls outside the given buffers. */
+typedef enum dg_dtype {
+  DG_F32 = 0,
+  DG_F16 = 1,
+  DG_BF16 = 2,
+  DG_F8E4M3 = 3 /* OCP 8-bit float: 4 exponent bits, 3 mantissa bits, largest 448 */
+} dg_dtype;
+
+#define DG_MAX_COLS 65536    /* columns of a row of dg_embed_rows, dg_norm_rows */
+#define DG_MAX_HEADS 1024    /* query heads of dg_attend_edges */
+#define DG_MAX_HEAD_DIM 256  /* elements of a head */
+
+/* Embedding rows: out[i] = scale * row_scale[ids[i]] * table[ids[i]], i in [0, n).
+ *   table      [N] rows of D elements of table_type (any dg_dtype).
+ *   row_scale  [N] float or NULL (all 1): for tables kept in 8 bits with a scale per
+ *              row, as dg_norm_rows writes them.
+ *   ids        [n] int32 in [0, N); -1 gives a zero row (an entry of a padded list), and
+ *              so does any other ID out of range, which also sets status.
+ *   out        [n] rows of out_type (DG_F32, DG_F16 or DG_BF16).
+ * DG_EINVAL for bad sizes or types, null pointers or an output that overlaps an input. */
+int dg_embed_rows(const void *table, int32_t table_type, int64_t N, int64_t D,
+                  int64_t table_stride, const float *row_scale, const int32_t *ids, int64_t n,
+                  float scale, void *out, int32_t out_type, int64_t out_stride, int32_t *status,
+                  hipStream_t stream);
+
+/* Workspace bytes of dg_embed_rows_grad for lists of up to n entries. */
+size_t dg_embed_rows_grad_workspace_bytes(int64_t N, int64_t D, int64_t n, int32_t sparse);
+
+/* Gradient of dg_embed_rows towards the table:
+ *   G[t] = scale * sum over i with ids[i] = t of grad_out[i],
+ * added in the order of the list, without atomics (the list is sorted by ID).
+ *   grad_out   [n] rows of D elements of `type`.
+ *   ids        as in the lookup; entries of -1 or out of range are left out.
+ *   rows, num_rows  both NULL: grad is the whole gradient, [N*D] elements of grad_type,
+ *              with zero rows for nodes that do not occur.  Otherwise rows receives the
+ *              nodes that occur, ascending, num_rows (device int64) their number u, and
+ *              grad row j the sum of node rows[j]; both have room for min(n, N) rows and
+ *              nothing is written past the first u.
+ * DG_EINVAL as above, DG_EWORKSPACE for a missing, small or misaligned workspace. */
+int dg_embed_rows_grad(const void *grad_out, int32_t type, int64_t grad_stride,
+                       const int32_t *ids, int64_t n, int64_t N, int64_t D, float scale, void *grad,
+                       int32_t grad_type, int32_t *rows, int64_t *num_rows, int32_t *status,
+                       void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Root-mean-square norm of n rows of D elements of `type`:
+ *   h = x + residual (residual NULL: h = x),  rstd = (mean(h^2) + eps)^(-1/2),
+ *   y = h * rstd * weight.
+ *   weight  [D] float.
+ *   y       [n*D]: of `type`, or of DG_F8E4M3 with scales: for each row (group = 0) or
+ *           each group of 32, 64 or 128 columns, scales [n*ceil(D/group)] (or [n])
+ *           receives c = max|y| / 448 and y its codes, y ~ code * c; a group of zeros
+ *           has c = 0 and codes 0.  A NaN makes its group's scale and codes NaN.
+ *   h       optional [n*D] of `type`: the sum, for the next residual and the gradient
+ *           (may be x or residual itself if that is contiguous).  The norm is taken of
+ *           the sum before its rounding.
+ *   rstd    optional [n] float, for the gradient.
+ * DG_EINVAL for bad sizes, types or groups, eps < 0 or NaN, null pointers or overlap. */
+int dg_norm_rows(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride,
+                 int32_t type, int64_t n, int64_t D, const float *weight, float eps, void *y,
+                 int32_t y_type, int32_t group, float *scales, void *h, float *rstd,
+                 hipStream_t stream);
+
+size_t dg_norm_rows_grad_workspace_bytes(int64_t n, int64_t D);
+
+/* Gradient of dg_norm_rows (an 8-bit y counts as y itself), from h and rstd as the
+ * forward call wrote them: with u = h * rstd and g = weight * grad_y,
+ *   grad_x = rstd * (g - u * mean(g * u)) + grad_h   [n*D] of `type`; it is also the
+ *            residual's gradient.  grad_h (optional): the gradient that reaches h itself.
+ *   grad_weight = sum over rows of grad_y * u        [D] float.
+ * grad_x may be grad_y or grad_h itself if that is contiguous. */
+int dg_norm_rows_grad(const void *grad_y, int64_t grad_stride, const void *h, int64_t h_stride,
+                      const float *rstd, const float *weight, const void *grad_h,
+                      int64_t grad_h_stride, int32_t type, int64_t n, int64_t D, void *grad_x,
+                      float *grad_weight, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Offsets of an edge list that is sorted by row, as dg_sample_group lists edges by
+ * frontier position (edge_src) without DG_SAMPLE_LAYERED, and within each hop with it:
+ *   offsets[r] = number of edges whose row is below r, r = 0 .. num_rows.
+ *   edge_src   [num_edges] int32, not decreasing, in [0, num_rows).
+ *   offsets    [num_rows + 1] int64. */
+int dg_edge_offsets(const int32_t *edge_src, int64_t num_edges, int64_t num_rows, int64_t *offsets,
+                    int32_t *status, hipStream_t stream);
+
+/* Workspace bytes of dg_attend_edges. */
+size_t dg_attend_edges_workspace_bytes(int64_t num_edges, int32_t heads, int32_t D);
+
+/* Attention of nq rows over lists of neighbours: with e in [offsets[i], offsets[i+1]),
+ * j = indices[e] and the head's key head (heads / kv_heads consecutive heads share one),
+ *   s_e = scale * q[i] . k[j] + bias[e],
+ *   lse[i] = ln(sum of exp(s_e)),   out[i] = sum of exp(s_e - lse[i]) * v[j].
+ *   q          [nq] rows of heads*D elements; k, v [nkv] rows of kv_heads*D elements.
+ *   offsets, indices  the lists: the sampled neighbours (dg_edge_offsets, edge_dst), or a
+ *              graph's own CSR arrays for all neighbours; offsets[0] = 0, offsets[nq] =
+ *              num_edges.  An index of -1 is no neighbour.  Lists may have any length.
+ *   bias       optional float [num_edges*bias_heads], bias_heads 1 (the same for all
+ *              heads) or heads: logarithms of edge weights, or -inf for an edge that is
+ *              masked, which adds nothing whatever its key and value rows hold.
+ *   out        [nq*heads*D] of `type`;  lse [nq*heads] float.  A row whose list is empty
+ *              or wholly masked has out = 0 and lse = -inf.
+ * DG_EINVAL for bad sizes or types, null pointers or overlap; DG_EWORKSPACE as above. */
+int dg_attend_edges(const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                    const void *v, int64_t v_stride, int32_t type, int64_t nq, int64_t nkv,
+                    int32_t heads, int32_t kv_heads, int32_t D, const int64_t *offsets,
+                    const int32_t *indices, int64_t num_edges, const float *bias,
+                    int32_t bias_heads, float scale, void *out, float *lse, int32_t *status,
+                    void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes of dg_attend_edges_grad. */
+size_t dg_attend_edges_grad_workspace_bytes(int64_t num_edges, int64_t nkv, int32_t heads,
+                                            int32_t kv_heads, int32_t D);
+
+/* Gradient of dg_attend_edges; the probabilities are recomputed from lse.
+ *   grad_out, out  [nq] rows of heads*D elements, lse [nq*heads]: the result's gradient
+ *              and the forward call's results.
+ *   grad_q [nq*heads*D], grad_k, grad_v [nkv*kv_heads*D]  of `type`: rows without an edge
+ *              are zeros.
+ *   grad_bias  optional float [num_edges*bias_heads] (needs bias): 0 at masked edges. */
+int dg_attend_edges_grad(const void *grad_out, int64_t grad_stride, const void *q,
+                         int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                         int64_t v_stride, const void *out, int64_t out_stride, const float *lse,
+                         int32_t type, int64_t nq, int64_t nkv, int32_t heads, int32_t kv_heads,
+                         int32_t D, const int64_t *offsets, const int32_t *indices,
+                         int64_t num_edges, const float *bias, int32_t bias_heads, float scale,
+                         void *grad_q, void *grad_k, void *grad_v, float *grad_bias,
+                         int32_t *status, void *ws, size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -17,12 +17,16 @@ import torch
 from . import _lib
 from ._lib import (DG_ECAPACITY, DG_MAX_BATCHES, DG_OK, DGError, Csr, Sizes, Timing, check,
                    load)
+from .rows import (AttendGrads, AttendResult, NormResult, attend_edges, attend_edges_grad,
+                   edge_offsets, embed_rows, embed_rows_grad, norm_rows, norm_rows_grad)
 
 __all__ = ["sample_bounds", "member_lines_bytes", "sample_group", "pack_group",
            "sample_pack_group", "assemble_batch",
            "assemble_batches", "cache_by_frequency",
-           "gather_rows", "pack_individual", "minhash_order", "DGError", "SampleResult",
-           "PackResult", "version"]
+           "gather_rows", "pack_individual", "minhash_order", "embed_rows", "embed_rows_grad",
+           "norm_rows", "norm_rows_grad", "edge_offsets", "attend_edges", "attend_edges_grad",
+           "DGError", "SampleResult", "PackResult", "NormResult", "AttendResult", "AttendGrads",
+           "version"]
 
 _L = load()
 

@@ -20,6 +20,7 @@ DG_PACK_ROWS_STREAM = 2
 DG_PACK_LOC_PENDING = 4
 DG_LOC_PENDING = 0x7fffffff
 DG_MAX_BATCHES = 64
+DG_F32, DG_F16, DG_BF16, DG_F8E4M3 = 0, 1, 2, 3
 STATUS_NAMES = {0: "DG_OK", -1: "DG_EINVAL", -2: "DG_ECAPACITY", -3: "DG_EHIP",
                 -4: "DG_EWORKSPACE"}
 
@@ -28,6 +29,7 @@ I32 = ctypes.c_int32
 U64 = ctypes.c_uint64
 U32 = ctypes.c_uint32
 VP = ctypes.c_void_p
+F32 = ctypes.c_float
 SZ = ctypes.c_size_t
 I32P = ctypes.POINTER(ctypes.c_int32)
 I64P = ctypes.POINTER(ctypes.c_int64)
@@ -92,6 +94,24 @@ SIGNATURES = {
     "dg_gather_rows": (ctypes.c_int, [VP, I64, I64, VP, I64, VP, VP, VP]),
     "dg_minhash_workspace_bytes": (SZ, [I64]),
     "dg_minhash_order": (ctypes.c_int, [VP, I64, I32, VP, I64, VP, I32, VP, VP, VP, SZ, VP]),
+    "dg_embed_rows": (ctypes.c_int, [VP, I32, I64, I64, I64, VP, VP, I64, F32, VP, I32, I64, VP,
+                                     VP]),
+    "dg_embed_rows_grad_workspace_bytes": (SZ, [I64, I64, I64, I32]),
+    "dg_embed_rows_grad": (ctypes.c_int, [VP, I32, I64, VP, I64, I64, I64, F32, VP, I32, VP, VP,
+                                          VP, VP, SZ, VP]),
+    "dg_norm_rows": (ctypes.c_int, [VP, I64, VP, I64, I32, I64, I64, VP, F32, VP, I32, I32, VP, VP,
+                                    VP, VP]),
+    "dg_norm_rows_grad_workspace_bytes": (SZ, [I64, I64]),
+    "dg_norm_rows_grad": (ctypes.c_int, [VP, I64, VP, I64, VP, VP, VP, I64, I32, I64, I64, VP, VP,
+                                         VP, SZ, VP]),
+    "dg_edge_offsets": (ctypes.c_int, [VP, I64, I64, VP, VP, VP]),
+    "dg_attend_edges_workspace_bytes": (SZ, [I64, I32, I32]),
+    "dg_attend_edges": (ctypes.c_int, [VP, I64, VP, I64, VP, I64, I32, I64, I64, I32, I32, I32, VP,
+                                       VP, I64, VP, I32, F32, VP, VP, VP, VP, SZ, VP]),
+    "dg_attend_edges_grad_workspace_bytes": (SZ, [I64, I64, I32, I32, I32]),
+    "dg_attend_edges_grad": (ctypes.c_int, [VP, I64, VP, I64, VP, I64, VP, I64, VP, I64, VP, I32,
+                                            I64, I64, I32, I32, I32, VP, VP, I64, VP, I32, F32, VP,
+                                            VP, VP, VP, VP, VP, SZ, VP]),
 }
 
 _lib = None

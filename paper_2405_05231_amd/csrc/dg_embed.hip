@@ -1,0 +1,362 @@
+// Rows of an embedding table for a list of nodes, scaled, and the gradient of that
+// lookup: one sum per node over the list entries that hold it.
+//
+//   forward   y_i = a r[id_i] T[id_i]           (r: a scale per row, optional)
+//   gradient  G[t] = a sum over i with id_i = t of dy_i
+//
+// Both move rows and compute next to nothing (one or two operations per element), so
+// both are bound by memory.
+#include <string.h>
+
+#include "dg_segments.h"
+
+namespace dg {
+namespace {
+
+constexpr int ET = 256;
+constexpr int EU = 4;  // vectors per thread (forward), rows in flight per lane (gradient)
+
+// ------------------------------------------------------------------ forward
+// The output is one run of vectors, vpr per row, and a thread takes one of each of
+// the EU slices of its block's tile: no lane idles whatever the row length, where a
+// power of two lanes per row would leave a quarter of them idle at 768 values.
+template <typename T, typename TO, int V, bool NT>
+__global__ __launch_bounds__(ET) void k_embed_rows(const T *table, int64_t N, int cols,
+                                                   int64_t stride, const float *row_scale,
+                                                   const int32_t *ids, int64_t n, float scale,
+                                                   TO *out, int64_t out_stride, uint32_t vpr,
+                                                   uint32_t magic, int32_t *status) {
+  const uint64_t v0 = (uint64_t)blockIdx.x * (ET * EU);
+  const int64_t row0 = (int64_t)(v0 / vpr);
+  const uint32_t rem = (uint32_t)(v0 - (uint64_t)row0 * vpr);
+  int64_t row[EU];
+  int c[EU];
+  int32_t id[EU];
+#pragma unroll
+  for (int u = 0; u < EU; ++u) {
+    // vpr 2 to 1024: exact by the multiplication, since at < 2^12 and vpr * at < 2^32;
+    // longer rows: a tile spans two at most
+    const uint32_t at = rem + u * ET + threadIdx.x;
+    const uint32_t q = magic ? __umulhi(at, magic) : vpr == 1 ? at : (uint32_t)(at >= vpr);
+    row[u] = row0 + q;
+    c[u] = (int)(at - q * vpr);
+    id[u] = ids[min(row[u], n - 1)];
+  }
+  Raw<T, V> x[EU];
+  float f[EU];
+  bool bad = false;
+#pragma unroll
+  for (int u = 0; u < EU; ++u) {
+    const bool ok = id[u] >= 0 && (int64_t)id[u] < N;
+    bad |= !ok && id[u] != -1;
+    const int64_t r = ok ? id[u] : 0;
+    x[u] = ld_piece<T, V>(table + r * stride, Piece<V>(c[u], cols));
+    f[u] = row_scale ? row_scale[r] * scale : scale;
+    if (!ok) {
+      memset(&x[u], 0, sizeof(x[u]));
+      f[u] = 0.f;
+    }
+  }
+  if (bad && status) atomicOr(status, 1);
+#pragma unroll
+  for (int u = 0; u < EU; ++u) {
+    if (row[u] >= n) continue;
+    float y[V];
+    to_floats<T, V>(x[u], y);
+#pragma unroll
+    for (int i = 0; i < V; ++i) y[i] *= f[u];
+    st_piece<NT>(from_floats<TO, V>(y), out + row[u] * out_stride, Piece<V>(c[u], cols));
+  }
+}
+
+// Outputs of more bytes than this leave the caches anyway (256 MB at the last level).
+constexpr int64_t NT_BYTES = 320 * 1000 * 1000;
+
+template <typename T, typename TO, int V>
+int launch_rows(const void *table, int64_t N, int cols, int64_t stride, const float *row_scale,
+                const int32_t *ids, int64_t n, float scale, void *out, int64_t out_stride,
+                int32_t *status, hipStream_t s) {
+  const uint32_t vpr = (uint32_t)((cols + V - 1) / V);
+  const uint32_t magic =
+      vpr == 1 || vpr > 1024 ? 0u : (uint32_t)(((1ull << 32) + vpr - 1) / vpr);
+  const int64_t blocks = (n * (int64_t)vpr + ET * EU - 1) / (ET * EU);
+  if (blocks > 0x7fffffffll)
+    return set_error(DG_EINVAL, "dg_embed_rows: n * D is too large");
+  const bool nt = n * cols * (int64_t)sizeof(TO) > NT_BYTES && cols % V == 0;
+  auto go = [&](auto flag) {
+    hipLaunchKernelGGL((k_embed_rows<T, TO, V, decltype(flag)::value>), dim3((unsigned)blocks),
+                       dim3(ET), 0, s, (const T *)table, N, cols, stride, row_scale, ids, n,
+                       scale, (TO *)out, out_stride, vpr, magic, status);
+  };
+  if (nt) go(std::true_type());
+  else go(std::false_type());
+  DG_HIP(hipGetLastError());
+  return DG_OK;
+}
+
+// ------------------------------------------------------------------ gradient
+// A group of 2^lg lanes adds the entries of one chunk of the sorted list, a vector
+// of columns each (dg_segments.h); blocks from sum_blocks on write the rows of nodes
+// that do not occur as zeros (a gradient in full).
+template <typename T, typename TO, int V>
+__global__ __launch_bounds__(ET) void k_embed_sum(IdSort a, uint32_t limit, const T *src,
+                                                  int64_t stride, int cols, float scale, TO *out,
+                                                  int64_t out_stride, int lg,
+                                                  int64_t sum_blocks) {
+  const int sub = threadIdx.x & ((1 << lg) - 1);
+  const Piece<V> pc((blockIdx.y << lg) + sub, cols);
+  const int per = ET >> lg;
+  if ((int64_t)blockIdx.x >= sum_blocks) {
+    const int64_t groups = ((int64_t)gridDim.x - sum_blocks) * per;
+    const float zero[V] = {};
+    for (int64_t r = ((int64_t)blockIdx.x - sum_blocks) * per + (threadIdx.x >> lg); r < a.slots;
+         r += groups)
+      if (!a.seen[r]) st_piece<false>(from_floats<TO, V>(zero), out + r * out_stride, pc);
+    return;
+  }
+  const int64_t c = (int64_t)blockIdx.x * per + (threadIdx.x >> lg);
+  if (c >= a.chunks) return;
+  const Chunk k = chunk_of(a.dst, a.n, a.C, c);
+  const int64_t end = k.beyond ? min(k.stop + a.C, a.n) : k.stop;
+  float acc[V];
+  int32_t cur = -1;
+  bool lead = k.lead_part;
+  auto flush = [&](bool final) {
+    if ((uint32_t)cur >= limit) return;
+    const bool part = lead || (final && k.trail_part);
+    if (part) {
+      float *p = a.part + (2 * c + (lead ? 0 : 1)) * a.width;
+      Raw<float, V> r;
+      memcpy(&r.w, acc, sizeof(acc));
+      st_piece<false>(r, p, pc);
+      if (!lead && sub == 0 && blockIdx.y == 0) a.long_at[atomicAdd(a.n_long, 1)] = (int32_t)c;
+    } else {
+      float y[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) y[i] = acc[i] * scale;
+      st_piece<false>(from_floats<TO, V>(y), out + (int64_t)cur * out_stride, pc);
+    }
+    lead = false;
+  };
+  bool done = false;
+  for (int64_t i = k.begin; i < end && !done; i += EU) {
+    int32_t d[EU];
+    Raw<T, V> x[EU];
+#pragma unroll
+    for (int u = 0; u < EU; ++u) {
+      const int64_t j = min(i + u, a.n - 1);
+      d[u] = a.dst[j];
+      x[u] = ld_piece<T, V>(src + (int64_t)a.order[j] * stride, pc);
+    }
+#pragma unroll
+    for (int u = 0; u < EU; ++u) {
+      if (done || i + u >= end || (i + u >= k.stop && d[u] != k.last)) {
+        done = true;
+        continue;
+      }
+      float y[V];
+      to_floats<T, V>(x[u], y);
+      if (i + u == k.begin || d[u] != cur) {
+        if (i + u != k.begin) flush(false);
+        cur = d[u];
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = y[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] += y[e];
+      }
+    }
+  }
+  if (k.begin < end) flush(true);
+}
+
+// A block per long segment: its groups of lanes add every NG-th partial sum, then one
+// group adds theirs in order.
+template <typename TO, int V>
+__global__ __launch_bounds__(ET) void k_join(IdSort a, JoinOut o, int cols, int lg) {
+  __shared__ float s_sum[ET * V];
+  const int z = blockIdx.z;
+  const int sub = threadIdx.x & ((1 << lg) - 1), g = threadIdx.x >> lg, groups = ET >> lg;
+  const Piece<V> pc((blockIdx.y << lg) + sub, cols);
+  const int many = *a.n_long;
+  for (int l = blockIdx.x; l < many; l += gridDim.x) {
+    const int64_t c = a.long_at[l];
+    const int32_t node = a.dst[(c + 1) * a.C - 1];
+    // last chunk that starts with the node: chunk c + 1 does
+    int64_t lo = c + 1, hi = a.chunks;
+    while (hi - lo > 1) {
+      const int64_t step = (hi - lo + ET - 1) / ET;
+      const int64_t at = lo + (int64_t)threadIdx.x * step;
+      const int ok = __syncthreads_count(at < hi && a.dst[at * a.C] == node);
+      lo += (int64_t)(ok - 1) * step;
+      hi = min(hi, lo + step);
+    }
+    const int64_t parts = lo - c + 1;
+    float acc[V] = {};
+    for (int64_t j0 = g; j0 < parts; j0 += 4 * groups) {
+      Raw<float, V> x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t j = min(j0 + u * groups, parts - 1);
+        const int64_t slot = j == 0 ? 2 * c + 1 : 2 * (c + j);
+        x[u] = ld_piece<float, V>(a.part + slot * a.width + o.at[z], pc);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (j0 + u * groups >= parts) continue;
+        float y[V];
+        to_floats<float, V>(x[u], y);
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] += y[e];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) s_sum[(e * groups + g) * (1 << lg) + sub] = acc[e];
+    __syncthreads();
+    if (g == 0) {
+      float y[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float t = 0.f;
+        for (int q = 0; q < groups; ++q) t += s_sum[(e * groups + q) * (1 << lg) + sub];
+        y[e] = t * o.factor[z];
+      }
+      st_piece<false>(from_floats<TO, V>(y),
+                      static_cast<TO *>(o.out[z]) + (int64_t)node * o.stride[z], pc);
+    }
+    __syncthreads();
+  }
+}
+
+// Zero blocks: about eight rows for each group of lanes, at most 4096 blocks.
+int64_t zero_blocks(const IdSort &a, int lg) {
+  if (a.compact) return 0;
+  const int64_t b = (a.slots + 8 * (ET >> lg) - 1) / (8 * (ET >> lg));
+  return b > 4096 ? 4096 : b;
+}
+
+void set_sort(IdSort &a, const int32_t *ids, int64_t n, int64_t N, int64_t D, bool compact) {
+  memset(&a, 0, sizeof(a));
+  a.ids = ids;
+  a.n = n;
+  a.slots = N;
+  a.compact = compact;
+  a.width = D;
+}
+
+}  // namespace
+
+int run_join(const IdSort &a, const JoinOut &o, int outs, int cols, int32_t type, hipStream_t s) {
+  if (!a.part) return DG_OK;  // too short a list for a long segment
+  const int64_t most = a.chunks / 2 + 1;
+  return with_type(type, [&](auto t) {
+    using TO = decltype(t);
+    return with_vec<TO>(cols, [&](auto vec) {
+      constexpr int V = decltype(vec)::value;
+      const RowLanes r = row_lanes((cols + V - 1) / V);
+      hipLaunchKernelGGL((k_join<TO, V>),
+                         dim3((unsigned)(most > 512 ? 512 : most), (unsigned)r.tiles,
+                              (unsigned)outs),
+                         dim3(ET), 0, s, a, o, cols, r.lg);
+      DG_HIP(hipGetLastError());
+      return (int)DG_OK;
+    });
+  });
+}
+
+}  // namespace dg
+
+using namespace dg;
+
+extern "C" int dg_embed_rows(const void *table, int32_t table_type, int64_t N, int64_t D,
+                             int64_t table_stride, const float *row_scale, const int32_t *ids,
+                             int64_t n, float scale, void *out, int32_t out_type,
+                             int64_t out_stride, int32_t *status, hipStream_t stream) {
+  if (n < 0 || N < 1 || N > 0x7fffffffll || D < 1 || D > DG_MAX_COLS || table_stride < D ||
+      out_stride < D)
+    return set_error(DG_EINVAL, "dg_embed_rows: bad sizes");
+  if (!type_bytes(table_type) || !is_wide_type(out_type))
+    return set_error(DG_EINVAL, "dg_embed_rows: bad types");
+  if (n == 0) return DG_OK;
+  if (!table || !ids || !out)
+    return set_error(DG_EINVAL, "dg_embed_rows: null pointer argument");
+  const int64_t out_bytes = span_bytes(n, D, out_stride, type_bytes(out_type));
+  if (ranges_overlap(out, out_bytes, table, span_bytes(N, D, table_stride, type_bytes(table_type))) ||
+      ranges_overlap(out, out_bytes, ids, 4 * n) || ranges_overlap(out, out_bytes, row_scale, 4 * N))
+    return set_error(DG_EINVAL, "dg_embed_rows: the output overlaps an input");
+  auto to = [&](auto in) {
+    return with_type(out_type, [&](auto o) {
+      using T = decltype(in);
+      using TO = decltype(o);
+      constexpr int V = 16 / (int)(sizeof(T) > sizeof(TO) ? sizeof(T) : sizeof(TO));
+      auto go = [&](auto v) {
+        return launch_rows<T, TO, decltype(v)::value>(table, N, (int)D, table_stride, row_scale,
+                                                      ids, n, scale, out, out_stride, status,
+                                                      stream);
+      };
+      return D >= V ? go(std::integral_constant<int, V>()) : go(std::integral_constant<int, 1>());
+    });
+  };
+  if (table_type == DG_F8E4M3) return to(e4m3());
+  return with_type(table_type, to);
+}
+
+extern "C" size_t dg_embed_rows_grad_workspace_bytes(int64_t N, int64_t D, int64_t n,
+                                                     int32_t sparse) {
+  if (n < 0 || n > 0x7fffffffll || N < 1 || N > 0x7fffffffll || D < 1 || D > DG_MAX_COLS) return 0;
+  IdSort a;
+  set_sort(a, nullptr, n, N, D, sparse != 0);
+  return sort_room(a);
+}
+
+extern "C" int dg_embed_rows_grad(const void *grad_out, int32_t type, int64_t grad_stride,
+                                  const int32_t *ids, int64_t n, int64_t N, int64_t D, float scale,
+                                  void *grad, int32_t grad_type, int32_t *rows, int64_t *num_rows,
+                                  int32_t *status, void *ws, size_t ws_bytes, hipStream_t stream) {
+  if (n < 0 || n > 0x7fffffffll || N < 1 || N > 0x7fffffffll || D < 1 || D > DG_MAX_COLS ||
+      grad_stride < D)
+    return set_error(DG_EINVAL, "dg_embed_rows_grad: bad sizes");
+  if (!is_wide_type(type) || !is_wide_type(grad_type))
+    return set_error(DG_EINVAL, "dg_embed_rows_grad: bad types");
+  if ((rows != nullptr) != (num_rows != nullptr))
+    return set_error(DG_EINVAL, "dg_embed_rows_grad: rows and num_rows come together");
+  const bool sparse = rows != nullptr;
+  if (n > 0 && (!grad_out || !ids))
+    return set_error(DG_EINVAL, "dg_embed_rows_grad: null pointer argument");
+  if (!grad && !(sparse && n == 0))
+    return set_error(DG_EINVAL, "dg_embed_rows_grad: null pointer argument");
+  const int64_t out_rows = sparse ? (n < N ? n : N) : N;
+  const int64_t out_bytes = out_rows * D * type_bytes(grad_type);
+  if (ranges_overlap(grad, out_bytes, grad_out, span_bytes(n, D, grad_stride, type_bytes(type))) ||
+      ranges_overlap(grad, out_bytes, ids, 4 * n) || ranges_overlap(rows, 4 * out_rows, ids, 4 * n))
+    return set_error(DG_EINVAL, "dg_embed_rows_grad: an output overlaps an input");
+  IdSort a;
+  set_sort(a, ids, n, N, D, sparse);
+  Carve size(nullptr);
+  carve_sort(a, size);
+  if (!ws || ws_bytes < size.used || ((uintptr_t)ws & 255))
+    return set_error(DG_EWORKSPACE, "dg_embed_rows_grad: workspace needs %zu bytes", size.used);
+  Carve c(ws);
+  carve_sort(a, c);
+  DG_TRY(run_sort(a, rows, num_rows, status, stream));
+  if (n == 0 && sparse) return DG_OK;
+  return with_type(type, [&](auto in) {
+    return with_type(grad_type, [&](auto o) {
+      using T = decltype(in);
+      using TO = decltype(o);
+      return with_vec<T>(D, [&](auto v) {
+        constexpr int V = decltype(v)::value;
+        const RowLanes r = row_lanes((D + V - 1) / V);
+        const int per = ET >> r.lg;
+        const int64_t sums = (a.chunks + per - 1) / per;
+        hipLaunchKernelGGL((k_embed_sum<T, TO, V>),
+                           dim3((unsigned)(sums + zero_blocks(a, r.lg)), (unsigned)r.tiles),
+                           dim3(ET), 0, stream, a, a.limit(), (const T *)grad_out, grad_stride,
+                           (int)D, scale, (TO *)grad, D, r.lg, sums);
+        DG_HIP(hipGetLastError());
+        const JoinOut j = {{grad, nullptr}, {D, 0}, {0, 0}, {scale, 0.f}};
+        return run_join(a, j, 1, (int)D, grad_type, stream);
+      });
+    });
+  });
+}

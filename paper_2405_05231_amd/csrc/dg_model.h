@@ -1,0 +1,281 @@
+// Device helpers shared by the operators on a model's rows (embedding rows, RMS
+// norm, neighbour attention): element types, vectors of them at any alignment,
+// and sums and maxima over aligned groups of lanes.  Arithmetic is in 32 bits;
+// values are rounded to their 16- or 8-bit type once, when they are stored.
+#pragma once
+
+#include <type_traits>
+
+#include "dg_common.h"
+
+namespace dg {
+
+// ---------------------------------------------------------------- element types
+struct e4m3 {
+  uint8_t bits;
+};
+
+inline int type_bytes(int32_t t) {
+  return t == DG_F32 ? 4 : t == DG_F16 || t == DG_BF16 ? 2 : t == DG_F8E4M3 ? 1 : 0;
+}
+inline bool is_wide_type(int32_t t) { return t == DG_F32 || t == DG_F16 || t == DG_BF16; }
+
+// Calls f with a value of the element type; f returns a status.
+template <typename F>
+inline int with_type(int32_t t, F f) {
+  if (t == DG_F32) return f(float());
+  if (t == DG_F16) return f(_Float16());
+  return f(__bf16());
+}
+
+// W bytes at any alignment (gfx950 takes global vectors at any byte address).
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+template <int W>
+struct Words;
+template <>
+struct Words<32> {
+  typedef uint32_t type __attribute__((ext_vector_type(8)));
+};
+template <>
+struct Words<16> {
+  typedef u32x4 type;
+};
+template <>
+struct Words<8> {
+  typedef u32x2 type;
+};
+template <>
+struct Words<4> {
+  typedef uint32_t type;
+};
+template <>
+struct Words<2> {
+  typedef uint16_t type;
+};
+template <>
+struct Words<1> {
+  typedef uint8_t type;
+};
+
+// V elements of type T as they lie in memory.
+template <typename T, int V>
+struct Raw {
+  typedef typename Words<sizeof(T) * V>::type W;
+  typedef W W_any __attribute__((aligned(1)));
+  W w;
+};
+
+template <typename T, int V>
+__device__ __forceinline__ Raw<T, V> ld_raw(const T *p) {
+  Raw<T, V> r;
+  r.w = *reinterpret_cast<const typename Raw<T, V>::W_any *>(p);
+  return r;
+}
+template <bool NT, typename T, int V>
+__device__ __forceinline__ void st_raw(Raw<T, V> r, T *p) {
+  auto *q = reinterpret_cast<typename Raw<T, V>::W_any *>(p);
+  if (NT) __builtin_nontemporal_store(r.w, q);
+  else *q = r.w;
+}
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(_Float16 x) { return (float)x; }
+__device__ __forceinline__ float to_f32(__bf16 x) { return (float)x; }
+__device__ __forceinline__ float to_f32(e4m3 x) {
+  return __builtin_amdgcn_cvt_f32_fp8((int)x.bits, 0);
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void to_floats(const Raw<T, V> &r, float (&x)[V]) {
+  if constexpr (std::is_same_v<T, e4m3>) {
+    if constexpr (V == 1) {
+      x[0] = __builtin_amdgcn_cvt_f32_fp8((int)r.w, 0);
+    } else {
+      uint32_t w[(V + 3) / 4];
+      __builtin_memcpy(w, &r.w, V);
+#pragma unroll
+      for (int i = 0; i < V; i += 4) {
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i / 4], false);
+        const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i / 4], true);
+        x[i] = lo[0];
+        x[i + 1] = lo[1];
+        x[i + 2] = hi[0];
+        x[i + 3] = hi[1];
+      }
+    }
+  } else {
+    T t[V];
+    __builtin_memcpy(t, &r.w, sizeof(T) * V);
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = to_f32(t[i]);
+  }
+}
+
+// Rounds to nearest, ties to even.
+template <typename T, int V>
+__device__ __forceinline__ Raw<T, V> from_floats(const float (&x)[V]) {
+  Raw<T, V> r;
+  if constexpr (std::is_same_v<T, e4m3>) {
+    if constexpr (V == 1) {
+      r.w = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[0], 0, false);
+    } else {
+      uint32_t w[(V + 3) / 4];
+#pragma unroll
+      for (int i = 0; i < V; i += 4) {
+        int v = __builtin_amdgcn_cvt_pk_fp8_f32(x[i], x[i + 1], 0, false);
+        w[i / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[i + 2], x[i + 3], v, true);
+      }
+      __builtin_memcpy(&r.w, w, V);
+    }
+  } else {
+    T t[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) t[i] = (T)x[i];
+    __builtin_memcpy(&r.w, t, sizeof(T) * V);
+  }
+  return r;
+}
+
+// Elements that one lane holds of a row: 16 bytes of a 32- or 16-bit type.
+template <typename T>
+constexpr int VEC = 16 / (int)sizeof(T);
+
+// A lane's share of a row of `cols` elements cut into vectors of V: vector c.
+// The last vector of a row whose length is no multiple of V starts at cols - V,
+// so that every vector is whole; elements before V*c belong to the vector before
+// (`own(i)` false) and lanes past the row own none.  A row shorter than V is read
+// element by element.
+template <int V>
+struct Piece {
+  int at;     // first element of the vector
+  int first;  // first element that is this lane's own
+  bool some;  // whether the lane owns any
+  __device__ __forceinline__ Piece(int c, int cols) {
+    const int want = c * V;
+    at = min(want, cols - V);
+    some = want < cols;
+    first = some ? want : cols;
+  }
+  __device__ __forceinline__ bool own(int i) const { return at + i >= first; }
+};
+
+template <typename T, int V>
+__device__ __forceinline__ Raw<T, V> ld_piece(const T *row, const Piece<V> &p) {
+  return ld_raw<T, V>(row + p.at);
+}
+// Stores a vector whose elements are right whoever owns them.
+template <bool NT, typename T, int V>
+__device__ __forceinline__ void st_piece(const Raw<T, V> &r, T *row, const Piece<V> &p) {
+  if (p.some) st_raw<NT>(r, row + p.at);
+}
+
+// Calls f with the elements per vector of rows of `cols` elements.
+template <typename T, typename F>
+inline int with_vec(int64_t cols, F f) {
+  using std::integral_constant;
+  if (cols >= VEC<T>) return f(integral_constant<int, VEC<T>>());
+  return f(integral_constant<int, 1>());
+}
+
+// ---------------------------------------------------------------- groups of lanes
+// Sums or maxima over lanes whose numbers agree outside bits from..to-1, to each of
+// them; the same in the whole wave, all of whose lanes take part.  Lanes 1, 2, 4 and
+// 8 apart meet by DPP, 16 and 32 apart by swapping halves of two registers.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u32(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+}
+__device__ __forceinline__ float as_f32(uint32_t x) { return __builtin_bit_cast(float, x); }
+__device__ __forceinline__ uint32_t as_u32(float x) { return __builtin_bit_cast(uint32_t, x); }
+
+struct AddF {
+  __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const {
+    return as_u32(as_f32(a) + as_f32(b));
+  }
+};
+struct MaxF {
+  __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const {
+    return as_u32(fmaxf(as_f32(a), as_f32(b)));
+  }
+};
+// Of magnitudes as bit patterns, in which NaN is above infinity and stays.
+struct MaxU {
+  __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const {
+    return max(a, b);
+  }
+};
+
+// Lanes 2^STEP apart.  FROM_0: the steps below are done, so that lanes agree within
+// 2^STEP and a mirror of 8 or 16 lanes does for steps 2 and 3.
+template <int STEP, bool FROM_0, typename Op>
+__device__ __forceinline__ uint32_t meet(uint32_t x, Op op) {
+  if constexpr (STEP == 0) {
+    return op(x, dpp_u32<0xB1>(x));  // quad_perm 1,0,3,2
+  } else if constexpr (STEP == 1) {
+    return op(x, dpp_u32<0x4E>(x));  // quad_perm 2,3,0,1
+  } else if constexpr (STEP == 2) {
+    if (FROM_0) return op(x, dpp_u32<0x141>(x));  // row_half_mirror
+    // row_shl:4 into the even quads of a row, row_shr:4 into the odd ones
+    int y = __builtin_amdgcn_update_dpp((int)x, (int)x, 0x104, 0xf, 0x5, false);
+    y = __builtin_amdgcn_update_dpp(y, (int)x, 0x114, 0xf, 0xa, false);
+    return op(x, (uint32_t)y);
+  } else if constexpr (STEP == 3) {
+    return op(x, FROM_0 ? dpp_u32<0x140>(x)    // row_mirror
+                        : dpp_u32<0x128>(x));  // row_ror:8
+  } else if constexpr (STEP == 4) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return op(r[0], r[1]);
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return op(r[0], r[1]);
+  }
+}
+template <bool FROM_0, int N, typename Op>
+__device__ __forceinline__ void lanes_reduce(uint32_t (&x)[N], int from, int to, Op op) {
+#define DG_MEET(S)                                                                  \
+  if (from <= S && to > S) {                                                        \
+    _Pragma("unroll") for (int i = 0; i < N; ++i) x[i] = meet<S, FROM_0>(x[i], op); \
+  }
+  DG_MEET(0)
+  DG_MEET(1)
+  DG_MEET(2)
+  DG_MEET(3)
+  DG_MEET(4)
+  DG_MEET(5)
+#undef DG_MEET
+}
+template <bool FROM_0, int N, typename Op>
+__device__ __forceinline__ void lanes_reduce(float (&x)[N], int from, int to, Op op) {
+  uint32_t u[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) u[i] = as_u32(x[i]);
+  lanes_reduce<FROM_0>(u, from, to, op);
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = as_f32(u[i]);
+}
+// Over aligned groups of 2^lg lanes.
+template <int N>
+__device__ __forceinline__ void group_sum(float (&x)[N], int lg) {
+  lanes_reduce<true>(x, 0, lg, AddF());
+}
+
+// Smallest k with 2^k >= x.
+inline int log2_up(int64_t x) {
+  int k = 0;
+  while ((1ll << k) < x) ++k;
+  return k;
+}
+
+inline bool ranges_overlap(const void *a, int64_t an, const void *b, int64_t bn) {
+  if (!a || !b || an <= 0 || bn <= 0) return false;
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + (uintptr_t)bn && y < x + (uintptr_t)an;
+}
+// Bytes from the first to the last element of `rows` rows of `cols` elements,
+// `stride` apart.
+inline int64_t span_bytes(int64_t rows, int64_t cols, int64_t stride, int64_t size) {
+  return rows < 1 ? 0 : ((rows - 1) * stride + cols) * size;
+}
+
+}  // namespace dg

@@ -1,0 +1,574 @@
+// Root-mean-square norm of rows, with the addition of a residual before it and an
+// output in the rows' type or in 8 bits with scales, and its gradient.
+//
+//   h = x + r;   rstd = (mean(h^2) + eps)^(-1/2);   y = h rstd w
+//   8 bits: per row, or per group of 32, 64 or 128 columns, c = max|y| / 448 and
+//   q = e4m3(y / c), so that y is about q c
+//   gradient, with u = h rstd and g = w dy:
+//   dx = rstd (g - u mean(g u)) + dh,   dw = sum over rows of dy u
+//
+// A few operations per element: bound by memory.  A row is held in registers between
+// its sum of squares and its output, so each input is read and each output written
+// once.
+#include <string.h>
+
+#include "dg_model.h"
+
+namespace dg {
+namespace {
+
+constexpr int NT = 256;           // threads
+constexpr float F8_TOP = 448.f;   // largest finite e4m3 value
+constexpr int NORM_MAX_NV = 4;    // vectors that a lane holds of a row
+
+struct Norm {
+  const void *x, *res;
+  int64_t n, x_stride, res_stride;
+  const float *w;
+  int cols, lg;        // lanes per row: 2^lg (one wave at most), or a block (wide rows)
+  int lg_group;        // lanes that share an 8-bit scale; 31: the row's
+  int groups;          // scales per row
+  float eps;
+  void *y;
+  float *scale;
+  void *h;             // optional
+  float *rstd;         // optional
+};
+
+// 8-bit codes of y by the group's largest magnitude `top` (as bits): q = y / c,
+// c = top / 448.  Below 2^-100 the reciprocal would overflow, so such groups are
+// multiplied by 2^100 first.
+__device__ __forceinline__ float code_factor(float top, float *lift) {
+  *lift = top < 0x1p-100f ? 0x1p100f : 1.f;
+  return top == 0.f ? 0.f : F8_TOP / (top * *lift);
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void store_own(const Raw<T, V> &r, T *row, const Piece<V> &p, int cols) {
+  if (!p.some) return;
+  if (p.first == p.at) {
+    st_raw<false>(r, row + p.at);
+    return;
+  }
+  T t[V];
+  memcpy(t, &r.w, sizeof(t));
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (p.own(i) && p.at + i < cols) row[p.at + i] = t[i];
+}
+
+// One vector's way from h to the outputs.  top: the largest |y| of the scale's group.
+template <typename T, typename TO, int V>
+__device__ __forceinline__ void put_y(const Norm &a, int64_t row, const Piece<V> &p, const float (&y)[V],
+                                      float top) {
+  TO *out = static_cast<TO *>(a.y) + row * a.cols;
+  if constexpr (std::is_same_v<TO, e4m3>) {
+    float lift;
+    const float f = code_factor(top, &lift);
+    float q[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) q[i] = y[i] * lift * f;
+    store_own(from_floats<e4m3, V>(q), out, p, a.cols);
+  } else {
+    store_own(from_floats<TO, V>(y), out, p, a.cols);
+  }
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void load_h(const Norm &a, int64_t row, const Piece<V> &p, float (&h)[V]) {
+  const auto rx = ld_piece<T, V>(static_cast<const T *>(a.x) + row * a.x_stride, p);
+  to_floats<T, V>(rx, h);
+  if (a.res) {
+    float r[V];
+    const auto rr = ld_piece<T, V>(static_cast<const T *>(a.res) + row * a.res_stride, p);
+    to_floats<T, V>(rr, r);
+#pragma unroll
+    for (int i = 0; i < V; ++i) h[i] += r[i];
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (!p.own(i) || p.at + i >= a.cols) h[i] = 0.f;  // another lane's, or none's
+}
+
+// y = h rstd w, and the largest |y| as bits (NaN above all).
+template <int V>
+__device__ __forceinline__ uint32_t weigh(const Norm &a, const Piece<V> &p, const float (&h)[V],
+                                          float rstd, float (&y)[V]) {
+  const auto rw = ld_piece<float, V>(a.w, p);
+  float w[V];
+  to_floats<float, V>(rw, w);
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    y[i] = h[i] * rstd * w[i];
+    if (!p.own(i) || p.at + i >= a.cols) y[i] = 0.f;  // (0 * inf of a foreign weight)
+    top = max(top, as_u32(y[i]) & 0x7fffffffu);
+  }
+  return top;
+}
+
+// Rows of up to 64 * NV vectors: 2^lg lanes each, NV vectors per lane.
+template <typename T, typename TO, int V, int NV>
+__global__ __launch_bounds__(NT) void k_norm(Norm a) {
+  constexpr bool Q = std::is_same_v<TO, e4m3>;
+  const int lanes = 1 << a.lg, sub = threadIdx.x & (lanes - 1);
+  const int64_t row = (int64_t)blockIdx.x * (NT >> a.lg) + (threadIdx.x >> a.lg);
+  const bool live = row < a.n;
+  const int64_t at = live ? row : a.n - 1;
+  float h[NV][V], ss[1] = {0.f};
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const Piece<V> p(j * lanes + sub, a.cols);
+    load_h<T, V>(a, at, p, h[j]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) ss[0] += h[j][i] * h[j][i];
+  }
+  group_sum(ss, a.lg);
+  const float rstd = 1.f / sqrtf(ss[0] / (float)a.cols + a.eps);
+  float y[NV][V];
+  uint32_t top[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const Piece<V> p(j * lanes + sub, a.cols);
+    top[j] = weigh<V>(a, p, h[j], rstd, y[j]);
+  }
+  if (Q) {
+    if (a.lg_group == 31) {
+#pragma unroll
+      for (int j = 1; j < NV; ++j) top[0] = max(top[0], top[j]);
+      uint32_t t[1] = {top[0]};
+      lanes_reduce<true>(t, 0, a.lg, MaxU());
+#pragma unroll
+      for (int j = 0; j < NV; ++j) top[j] = t[0];
+    } else {
+      lanes_reduce<true>(top, 0, a.lg_group, MaxU());
+    }
+  }
+  if (!live) return;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const Piece<V> p(j * lanes + sub, a.cols);
+    put_y<T, TO, V>(a, row, p, y[j], as_f32(top[j]));
+    if (a.h) store_own(from_floats<T, V>(h[j]), static_cast<T *>(a.h) + row * a.cols, p, a.cols);
+    if (Q) {
+      if (a.lg_group == 31) {
+        if (j == 0 && sub == 0) a.scale[row] = as_f32(top[0]) / F8_TOP;
+      } else if ((sub & ((1 << a.lg_group) - 1)) == 0) {
+        const int g = (j * lanes + sub) >> a.lg_group;
+        if (g < a.groups) a.scale[row * a.groups + g] = as_f32(top[j]) / F8_TOP;
+      }
+    }
+  }
+  if (a.rstd && sub == 0) a.rstd[row] = rstd;
+}
+
+// Wider rows: a block per row, which reads the row again (from the caches) for each
+// of the steps.
+template <typename T, typename TO>
+__global__ __launch_bounds__(NT) void k_norm_wide(Norm a) {
+  constexpr int V = VEC<T>;
+  constexpr bool Q = std::is_same_v<TO, e4m3>;
+  __shared__ float s_sum[NT / 64];
+  __shared__ uint32_t s_top[NT / 64];
+  const int64_t row = blockIdx.x;
+  const int vecs = (a.cols + V - 1) / V;
+  float ss[1] = {0.f}, h[V], y[V];
+  for (int c = threadIdx.x; c < vecs; c += NT) {
+    load_h<T, V>(a, row, Piece<V>(c, a.cols), h);
+#pragma unroll
+    for (int i = 0; i < V; ++i) ss[0] += h[i] * h[i];
+  }
+  group_sum(ss, 6);
+  if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = ss[0];
+  __syncthreads();
+  float sum = 0.f;
+#pragma unroll
+  for (int q = 0; q < NT / 64; ++q) sum += s_sum[q];
+  const float rstd = 1.f / sqrtf(sum / (float)a.cols + a.eps);
+  uint32_t top[1] = {0};
+  if (Q && a.lg_group == 31) {
+    for (int c = threadIdx.x; c < vecs; c += NT) {
+      const Piece<V> p(c, a.cols);
+      load_h<T, V>(a, row, p, h);
+      top[0] = max(top[0], weigh<V>(a, p, h, rstd, y));
+    }
+    lanes_reduce<true>(top, 0, 6, MaxU());
+    if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top[0];
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < NT / 64; ++q) top[0] = max(top[0], s_top[q]);
+    if (threadIdx.x == 0) a.scale[row] = as_f32(top[0]) / F8_TOP;
+  }
+  for (int c0 = 0; c0 < vecs; c0 += NT) {  // every lane takes part in the maxima
+    const int c = c0 + threadIdx.x;
+    const Piece<V> p(c, a.cols);
+    load_h<T, V>(a, row, p, h);
+    uint32_t t[1] = {weigh<V>(a, p, h, rstd, y)};
+    if (Q && a.lg_group != 31) {
+      lanes_reduce<true>(t, 0, a.lg_group, MaxU());
+      if (c < vecs && (c & ((1 << a.lg_group) - 1)) == 0)
+        a.scale[row * a.groups + (c >> a.lg_group)] = as_f32(t[0]) / F8_TOP;
+    } else {
+      t[0] = top[0];
+    }
+    put_y<T, TO, V>(a, row, p, y, as_f32(t[0]));
+    if (a.h) store_own(from_floats<T, V>(h), static_cast<T *>(a.h) + row * a.cols, p, a.cols);
+  }
+  if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+}
+
+// Lanes and vectors per lane for rows of `vecs` vectors: the fewest idle slots, more
+// lanes before more vectors per lane; false: wider than a wave holds.  A scale's group
+// lies within the lanes of one row.
+bool norm_shape(int vecs, int least_lg, int most_nv, int *lg, int *nv) {
+  int best = 1 << 30;
+  for (int l = 6; l >= least_lg; --l) {
+    const int per = (vecs + (1 << l) - 1) >> l;
+    if (per > most_nv) break;
+    if ((per << l) < best) {
+      best = per << l;
+      *lg = l;
+      *nv = per;
+    }
+  }
+  return best < (1 << 30);
+}
+
+// Calls f with the vectors per lane.
+template <typename F>
+void with_nv(int nv, F f) {
+  using std::integral_constant;
+  if (nv == 1) f(integral_constant<int, 1>());
+  else if (nv == 2) f(integral_constant<int, 2>());
+  else if (nv == 3) f(integral_constant<int, 3>());
+  else f(integral_constant<int, 4>());
+}
+
+template <typename T, typename TO>
+int launch_norm(Norm &a, int group, hipStream_t s) {
+  return with_vec<T>(a.cols, [&](auto v) {
+    constexpr int V = decltype(v)::value;
+    const int vecs = (a.cols + V - 1) / V;
+    const bool by_row = group == 0 || group >= a.cols;
+    a.groups = by_row ? 1 : (a.cols + group - 1) / group;
+    a.lg_group = by_row ? 31 : log2_up(group / V);
+    int nv;
+    if (!norm_shape(vecs, by_row ? 0 : a.lg_group, V == 1 ? 1 : NORM_MAX_NV, &a.lg, &nv)) {
+      hipLaunchKernelGGL((k_norm_wide<T, TO>), dim3((unsigned)a.n), dim3(NT), 0, s, a);
+    } else {
+      const int per = NT >> a.lg;
+      with_nv(nv, [&](auto k) {
+        hipLaunchKernelGGL((k_norm<T, TO, V, V == 1 ? 1 : decltype(k)::value>),
+                           dim3((unsigned)((a.n + per - 1) / per)), dim3(NT), 0, s, a);
+      });
+    }
+    DG_HIP(hipGetLastError());
+    return (int)DG_OK;
+  });
+}
+
+// ------------------------------------------------------------------ gradient
+struct NormGrad {
+  const void *dy, *h, *dh;
+  int64_t n, dy_stride, h_stride, dh_stride;
+  const float *rstd, *w;
+  int cols, lg, vecs;
+  void *dx;
+  float *part;      // [blocks][cols] sums of dy u over each block's rows
+  int64_t blocks;
+  float *dw;
+};
+
+template <typename T, int V>
+__device__ __forceinline__ void load_f(const void *p, int64_t row, int64_t stride,
+                                       const Piece<V> &pc, int cols, float (&x)[V]) {
+  const auto r = ld_piece<T, V>(static_cast<const T *>(p) + row * stride, pc);
+  to_floats<T, V>(r, x);
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (!pc.own(i) || pc.at + i >= cols) x[i] = 0.f;
+}
+
+// Blocks take rows in turn, so that each lane's columns stay its own and the weight's
+// gradient is summed in registers; a block's sums over its groups of lanes, then the
+// sums over blocks (k_norm_dw), run in a fixed order.
+template <typename T, int V, int NV>
+__global__ __launch_bounds__(NT) void k_norm_grad(NormGrad a) {
+  __shared__ float s_dw[NT * V];
+  const int lanes = 1 << a.lg, sub = threadIdx.x & (lanes - 1), g = threadIdx.x >> a.lg;
+  const int per = NT >> a.lg;
+  float w[NV][V], dw[NV][V];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const Piece<V> p(j * lanes + sub, a.cols);
+    load_f<float, V>(a.w, 0, 0, p, a.cols, w[j]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) dw[j][i] = 0.f;
+  }
+  // (a block's waves make the same number of rounds: every lane takes part in the sums)
+  for (int64_t r0 = (int64_t)blockIdx.x * per; r0 < a.n; r0 += a.blocks * per) {
+    const int64_t row = r0 + g;
+    const bool live = row < a.n;
+    const int64_t at = live ? row : a.n - 1;
+    const float rstd = a.rstd[at];
+    float gy[NV][V], u[NV][V], dot[1] = {0.f};
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const Piece<V> p(j * lanes + sub, a.cols);
+      load_f<T, V>(a.h, at, a.h_stride, p, a.cols, u[j]);
+      load_f<T, V>(a.dy, at, a.dy_stride, p, a.cols, gy[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        u[j][i] *= rstd;
+        if (live) dw[j][i] += gy[j][i] * u[j][i];
+        gy[j][i] *= w[j][i];
+        dot[0] += gy[j][i] * u[j][i];
+      }
+    group_sum(dot, a.lg);
+    const float mean = dot[0] / (float)a.cols;
+    if (!live) continue;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const Piece<V> p(j * lanes + sub, a.cols);
+      float d[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) d[i] = rstd * (gy[j][i] - u[j][i] * mean);
+      if (a.dh) {
+        float x[V];
+        load_f<T, V>(a.dh, row, a.dh_stride, p, a.cols, x);
+#pragma unroll
+        for (int i = 0; i < V; ++i) d[i] += x[i];
+      }
+      store_own(from_floats<T, V>(d), static_cast<T *>(a.dx) + row * a.cols, p, a.cols);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < V; ++i) s_dw[i * NT + threadIdx.x] = dw[j][i];
+    __syncthreads();
+    if (g == 0) {
+      float t[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        t[i] = 0.f;
+        for (int q = 0; q < per; ++q) t[i] += s_dw[i * NT + q * lanes + sub];
+      }
+      Raw<float, V> r;
+      memcpy(&r.w, t, sizeof(t));
+      store_own(r, a.part + (int64_t)blockIdx.x * a.cols, Piece<V>(j * lanes + sub, a.cols), a.cols);
+    }
+  }
+}
+
+// Rows wider than a wave holds: a block per row in turn; the weight's gradient is added
+// up in the block's own row of `part`.
+template <typename T>
+__global__ __launch_bounds__(NT) void k_norm_grad_wide(NormGrad a) {
+  constexpr int V = VEC<T>;
+  __shared__ float s_sum[NT / 64];
+  float *part = a.part + (int64_t)blockIdx.x * a.cols;
+  for (int c = threadIdx.x; c < a.cols; c += NT) part[c] = 0.f;
+  __syncthreads();
+  for (int64_t row = blockIdx.x; row < a.n; row += a.blocks) {
+    const float rstd = a.rstd[row];
+    float gy[V], u[V], w[V], dot[1] = {0.f};
+    for (int c = threadIdx.x; c < a.vecs; c += NT) {
+      const Piece<V> p(c, a.cols);
+      load_f<T, V>(a.h, row, a.h_stride, p, a.cols, u);
+      load_f<T, V>(a.dy, row, a.dy_stride, p, a.cols, gy);
+      load_f<float, V>(a.w, 0, 0, p, a.cols, w);
+#pragma unroll
+      for (int i = 0; i < V; ++i) dot[0] += gy[i] * w[i] * (u[i] * rstd);
+    }
+    group_sum(dot, 6);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = dot[0];
+    __syncthreads();
+    float mean = 0.f;
+#pragma unroll
+    for (int q = 0; q < NT / 64; ++q) mean += s_sum[q];
+    mean /= (float)a.cols;
+    for (int c = threadIdx.x; c < a.vecs; c += NT) {
+      const Piece<V> p(c, a.cols);
+      load_f<T, V>(a.h, row, a.h_stride, p, a.cols, u);
+      load_f<T, V>(a.dy, row, a.dy_stride, p, a.cols, gy);
+      load_f<float, V>(a.w, 0, 0, p, a.cols, w);
+      float d[V];
+      if (a.dh) {
+        load_f<T, V>(a.dh, row, a.dh_stride, p, a.cols, d);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) d[i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        u[i] *= rstd;
+        d[i] += rstd * (gy[i] * w[i] - u[i] * mean);
+        if (p.own(i) && p.at + i < a.cols) part[p.at + i] += gy[i] * u[i];  // this lane's column
+      }
+      store_own(from_floats<T, V>(d), static_cast<T *>(a.dx) + row * a.cols, p, a.cols);
+    }
+  }
+}
+
+// dw: a wave per 64 columns would leave the chip idle, so a block's 16 waves take
+// every 16th block's sums of 64 columns and are added in order.
+__global__ __launch_bounds__(1024) void k_norm_dw(const float *part, int64_t blocks, int cols,
+                                                  float *dw) {
+  __shared__ float s[16][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int c = blockIdx.x * 64 + lane;
+  float t = 0.f;
+  if (c < cols) {
+    for (int64_t b0 = w; b0 < blocks; b0 += 16 * 8) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int64_t b = b0 + u * 16;
+        x[u] = b < blocks ? part[b * cols + c] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) t += x[u];
+    }
+  }
+  s[w][lane] = t;
+  __syncthreads();
+  if (w == 0 && c < cols) {
+    float sum = 0.f;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) sum += s[q][lane];
+    dw[c] = sum;
+  }
+}
+
+// Blocks of the gradient: four to a CU, fewer for few rows.
+constexpr int64_t GRAD_BLOCKS = 1024;
+int64_t grad_blocks(int64_t n, int lg) {
+  const int64_t per = NT >> lg, b = (n + per - 1) / per;
+  return b > GRAD_BLOCKS ? GRAD_BLOCKS : b < 1 ? 1 : b;
+}
+
+template <typename T>
+int launch_norm_grad(NormGrad &a, hipStream_t s) {
+  return with_vec<T>(a.cols, [&](auto v) {
+    constexpr int V = decltype(v)::value;
+    a.vecs = (a.cols + V - 1) / V;
+    int nv;
+    if (!norm_shape(a.vecs, 0, V == 1 ? 1 : NORM_MAX_NV, &a.lg, &nv)) {
+      a.blocks = a.n > GRAD_BLOCKS ? GRAD_BLOCKS : a.n < 1 ? 1 : a.n;
+      hipLaunchKernelGGL(k_norm_grad_wide<T>, dim3((unsigned)a.blocks), dim3(NT), 0, s, a);
+    } else {
+      a.blocks = grad_blocks(a.n, a.lg);
+      with_nv(nv, [&](auto k) {
+        hipLaunchKernelGGL((k_norm_grad<T, V, V == 1 ? 1 : decltype(k)::value>),
+                           dim3((unsigned)a.blocks), dim3(NT), 0, s, a);
+      });
+    }
+    hipLaunchKernelGGL(k_norm_dw, dim3((unsigned)((a.cols + 63) / 64)), dim3(1024), 0, s, a.part,
+                       a.blocks, a.cols, a.dw);
+    DG_HIP(hipGetLastError());
+    return (int)DG_OK;
+  });
+}
+
+}  // namespace
+}  // namespace dg
+
+using namespace dg;
+
+extern "C" int dg_norm_rows(const void *x, int64_t x_stride, const void *residual,
+                            int64_t residual_stride, int32_t type, int64_t n, int64_t D,
+                            const float *weight, float eps, void *y, int32_t y_type, int32_t group,
+                            float *scales, void *h, float *rstd, hipStream_t stream) {
+  if (n < 0 || n > 0x7fffffffll || D < 1 || D > DG_MAX_COLS || x_stride < D ||
+      (residual && residual_stride < D))
+    return set_error(DG_EINVAL, "dg_norm_rows: bad sizes");
+  if (!is_wide_type(type) || (y_type != type && y_type != DG_F8E4M3))
+    return set_error(DG_EINVAL, "dg_norm_rows: bad types");
+  if (group != 0 && group != 32 && group != 64 && group != 128)
+    return set_error(DG_EINVAL, "dg_norm_rows: group must be 0, 32, 64 or 128");
+  if (!(eps >= 0.f)) return set_error(DG_EINVAL, "dg_norm_rows: eps must not be negative");
+  if (n == 0) return DG_OK;
+  const bool q = y_type == DG_F8E4M3;
+  if (!x || !weight || !y || (q && !scales))
+    return set_error(DG_EINVAL, "dg_norm_rows: null pointer argument");
+  const int64_t b = type_bytes(type), xb = span_bytes(n, D, x_stride, b);
+  const int64_t rb = span_bytes(n, D, residual_stride, b);
+  const int64_t yb = n * D * type_bytes(y_type), hb = n * D * b;
+  // (h may be x or the residual itself: each element is read before it is written)
+  const bool h_is_x = h == x && x_stride == D, h_is_r = h == residual && residual_stride == D;
+  if (ranges_overlap(y, yb, x, xb) || ranges_overlap(y, yb, residual, rb) ||
+      ranges_overlap(y, yb, weight, 4 * D) || ranges_overlap(y, yb, h, hb) ||
+      (!h_is_x && ranges_overlap(h, hb, x, xb)) ||
+      (!h_is_r && ranges_overlap(h, hb, residual, rb)))
+    return set_error(DG_EINVAL, "dg_norm_rows: an output overlaps an input or output");
+  Norm a;
+  memset(&a, 0, sizeof(a));
+  a.x = x;
+  a.res = residual;
+  a.n = n;
+  a.x_stride = x_stride;
+  a.res_stride = residual_stride;
+  a.w = weight;
+  a.cols = (int)D;
+  a.eps = eps;
+  a.y = y;
+  a.scale = scales;
+  a.h = h;
+  a.rstd = rstd;
+  return with_type(type, [&](auto t) {
+    using T = decltype(t);
+    return q ? launch_norm<T, e4m3>(a, group, stream) : launch_norm<T, T>(a, 0, stream);
+  });
+}
+
+extern "C" size_t dg_norm_rows_grad_workspace_bytes(int64_t n, int64_t D) {
+  if (n < 0 || n > 0x7fffffffll || D < 1 || D > DG_MAX_COLS) return 0;
+  return ((size_t)(n > GRAD_BLOCKS ? GRAD_BLOCKS : n < 1 ? 1 : n) * (size_t)D * 4 + 255) &
+         ~(size_t)255;
+}
+
+extern "C" int dg_norm_rows_grad(const void *grad_y, int64_t grad_stride, const void *h,
+                                 int64_t h_stride, const float *rstd, const float *weight,
+                                 const void *grad_h, int64_t grad_h_stride, int32_t type,
+                                 int64_t n, int64_t D, void *grad_x, float *grad_weight, void *ws,
+                                 size_t ws_bytes, hipStream_t stream) {
+  if (n < 0 || n > 0x7fffffffll || D < 1 || D > DG_MAX_COLS || grad_stride < D || h_stride < D ||
+      (grad_h && grad_h_stride < D))
+    return set_error(DG_EINVAL, "dg_norm_rows_grad: bad sizes");
+  if (!is_wide_type(type)) return set_error(DG_EINVAL, "dg_norm_rows_grad: bad types");
+  if (!weight || !grad_weight || (n > 0 && (!grad_y || !h || !rstd || !grad_x)))
+    return set_error(DG_EINVAL, "dg_norm_rows_grad: null pointer argument");
+  const int64_t b = type_bytes(type), xb = n * D * b;
+  const bool in_place = grad_x == grad_y && grad_stride == D;
+  const bool in_dh = grad_x == grad_h && grad_h_stride == D;
+  if ((!in_place && ranges_overlap(grad_x, xb, grad_y, span_bytes(n, D, grad_stride, b))) ||
+      ranges_overlap(grad_x, xb, h, span_bytes(n, D, h_stride, b)) ||
+      (!in_dh && ranges_overlap(grad_x, xb, grad_h, span_bytes(n, D, grad_h_stride, b))) ||
+      ranges_overlap(grad_weight, 4 * D, weight, 4 * D))
+    return set_error(DG_EINVAL, "dg_norm_rows_grad: an output overlaps an input");
+  const size_t need = dg_norm_rows_grad_workspace_bytes(n, D);
+  if (!ws || ws_bytes < need || ((uintptr_t)ws & 255))
+    return set_error(DG_EWORKSPACE, "dg_norm_rows_grad: workspace needs %zu bytes", need);
+  NormGrad a;
+  memset(&a, 0, sizeof(a));
+  a.dy = grad_y;
+  a.h = h;
+  a.dh = grad_h;
+  a.n = n;
+  a.dy_stride = grad_stride;
+  a.h_stride = h_stride;
+  a.dh_stride = grad_h_stride;
+  a.rstd = rstd;
+  a.w = weight;
+  a.cols = (int)D;
+  a.dx = grad_x;
+  a.part = static_cast<float *>(ws);
+  a.dw = grad_weight;
+  return with_type(type, [&](auto t) { return launch_norm_grad<decltype(t)>(a, stream); });
+}

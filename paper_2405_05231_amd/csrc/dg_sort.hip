@@ -1,0 +1,382 @@
+// Stable sort of a list of node IDs (dg_segments.h): least significant digit
+// first, up to 10 bits a pass.  A pass counts the digits of each tile, scans the
+// counts of each digit along the tiles, and places the tiles' entries; ranks inside a
+// wave come from ballots, so that equal IDs cost no atomics and keep their order.
+// Lists of up to SMALL entries are sorted by one block in shared memory.
+//
+// Bound by the launches below some 10^5 entries and by the scattered 8-byte writes of
+// the place pass above.
+#include "dg_segments.h"
+
+namespace dg {
+namespace {
+
+constexpr int ST = 256;            // threads of a tile's block
+constexpr int SW = ST / 64;
+constexpr int MAX_BITS = 10;       // of a digit
+constexpr int BINS = 1 << MAX_BITS;
+constexpr int SMALL = 2048;
+constexpr int HEADS = 1024;        // entries of a block of k_heads_*
+
+// Rounds of 64 entries that a wave takes of its tile: short tiles until they fill
+// the chip.
+int sort_rounds(int64_t n) { return n > (1 << 20) ? 16 : 4; }
+
+__device__ __forceinline__ int32_t sort_key(int32_t id, int64_t slots, bool *bad) {
+  const bool ok = id >= 0 && (int64_t)id < slots;
+  *bad |= !ok && id != -1;
+  return ok ? id : (int32_t)slots;
+}
+
+// Lanes of the wave with this lane's digit.
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, uint64_t act) {
+  uint64_t m = act;
+  for (int b = 0; b < bits; ++b) {
+    const bool one = (d >> b) & 1;
+    const uint64_t x = __ballot(one);
+    m &= one ? x : ~x;
+  }
+  return m;
+}
+
+struct Pass {
+  const int32_t *key, *pos;  // pos NULL: the list itself (key = ids)
+  int32_t *key_out, *pos_out;
+  int shift, bits;
+  int64_t tiles;
+};
+
+template <int R, bool FIRST>
+__global__ __launch_bounds__(ST) void k_sort_count(IdSort a, Pass p, int32_t *status) {
+  __shared__ uint32_t s_cnt[BINS];
+  const int bins = 1 << p.bits;
+  for (int i = threadIdx.x; i < bins; i += ST) s_cnt[i] = 0;
+  if (FIRST && blockIdx.x == 0 && threadIdx.x == 0) *a.n_long = 0;
+  __syncthreads();
+  const int64_t t0 = (int64_t)blockIdx.x * (ST * R);
+  int32_t k[R];
+  bool bad = false;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t i = t0 + r * ST + threadIdx.x;
+    k[r] = p.key[min(i, a.n - 1)];
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t i = t0 + r * ST + threadIdx.x;
+    if (i >= a.n) continue;
+    if (FIRST) {
+      k[r] = sort_key(k[r], a.slots, &bad);
+      if (!a.compact && k[r] < a.slots) a.seen[k[r]] = 1;
+    }
+    atomicAdd(&s_cnt[((uint32_t)k[r] >> p.shift) & (bins - 1)], 1u);
+  }
+  if (FIRST && bad && status) atomicOr(status, 1);
+  __syncthreads();
+  for (int i = threadIdx.x; i < bins; i += ST) a.cnt[(int64_t)i * p.tiles + blockIdx.x] = s_cnt[i];
+}
+
+// A wave per digit: exclusive scan of its counts along the tiles, in place.
+__global__ __launch_bounds__(ST) void k_sort_scan(IdSort a, int64_t tiles, int bins) {
+  const int lane = threadIdx.x & 63, d = blockIdx.x * SW + (threadIdx.x >> 6);
+  if (d >= bins) return;  // the same for the wave
+  uint32_t *p = a.cnt + (int64_t)d * tiles;
+  uint32_t carry = 0;
+  for (int64_t c = 0; c < tiles; c += 256) {  // four rounds' loads together
+    uint32_t v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t i = c + q * 64 + lane;
+      v[q] = i < tiles ? p[i] : 0u;
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t i = c + q * 64 + lane;
+      const uint32_t incl = (uint32_t)wave_incl_sum_i32((int32_t)v[q]);
+      if (i < tiles) p[i] = carry + incl - v[q];
+      carry += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+    }
+  }
+  if (lane == 0) a.tot[d] = carry;
+}
+
+template <int R, bool FIRST>
+__global__ __launch_bounds__(ST) void k_sort_place(IdSort a, Pass p) {
+  __shared__ uint32_t s_at[SW][BINS];  // next place of each wave's digits
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int bins = 1 << p.bits;
+  for (int i = threadIdx.x; i < SW * BINS; i += ST) (&s_at[0][0])[i] = 0;
+  __syncthreads();
+  const int64_t t0 = (int64_t)blockIdx.x * (ST * R) + w * (64 * R);
+  int32_t k[R], v[R];
+  uint32_t rank[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t i = min(t0 + r * 64 + lane, a.n - 1);
+    k[r] = p.key[i];
+    v[r] = FIRST ? (int32_t)i : p.pos[i];
+  }
+  uint32_t *at = s_at[w];  // this wave's own: its LDS operations run in order
+  const uint64_t lt = lanes_below();
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const bool in = t0 + r * 64 + lane < a.n;
+    bool bad = false;
+    if (FIRST) k[r] = sort_key(k[r], a.slots, &bad);
+    const uint32_t d = ((uint32_t)k[r] >> p.shift) & (bins - 1);
+    const uint64_t same = same_digit(d, p.bits, __ballot(in));
+    if (in) {
+      const uint32_t old = at[d];
+      rank[r] = old + __popcll(same & lt);
+      __builtin_amdgcn_wave_barrier();
+      if (__builtin_ctzll(same) == lane) at[d] = old + (uint32_t)__popcll(same);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
+  // digits' first places: each thread takes BINS / ST digits in a row
+  constexpr int PER = BINS / ST;
+  uint32_t t[PER];
+  int64_t sum = 0, all;
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    const int d = threadIdx.x * PER + q;
+    t[q] = d < bins ? a.tot[d] : 0u;
+    sum += t[q];
+  }
+  int64_t first = block_excl_scan<ST>(sum, &all);
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    const int d = threadIdx.x * PER + q;
+    if (d < bins) {
+      uint32_t next = (uint32_t)first + a.cnt[(int64_t)d * p.tiles + blockIdx.x];
+#pragma unroll
+      for (int j = 0; j < SW; ++j) {
+        const uint32_t own = s_at[j][d];
+        s_at[j][d] = next;
+        next += own;
+      }
+    }
+    first += t[q];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (t0 + r * 64 + lane >= a.n) continue;
+    const uint32_t d = ((uint32_t)k[r] >> p.shift) & (bins - 1);
+    const uint32_t to = at[d] + rank[r];
+    p.key_out[to] = k[r];
+    p.pos_out[to] = v[r];
+  }
+}
+
+// ------------------------------------------------------------------ distinct nodes
+// Whether sorted entry i is the first of its node.
+__device__ __forceinline__ bool is_head(const int32_t *key, int64_t i, int64_t n, int64_t slots) {
+  if (i >= n) return false;
+  const int32_t k = key[i];
+  return k < slots && (i == 0 || key[i - 1] != k);
+}
+
+__global__ __launch_bounds__(ST) void k_heads_count(IdSort a, const int32_t *key) {
+  const int64_t t0 = (int64_t)blockIdx.x * HEADS;
+  int mine = 0;
+#pragma unroll
+  for (int r = 0; r < HEADS / ST; ++r)
+    mine += is_head(key, t0 + r * ST + threadIdx.x, a.n, a.slots);
+  int64_t all;
+  (void)block_excl_scan<ST>(mine, &all);
+  if (threadIdx.x == 0) a.heads[blockIdx.x] = (int32_t)all;
+}
+
+__global__ __launch_bounds__(1024) void k_heads_scan(IdSort a, int64_t blocks, int64_t *count) {
+  int64_t carry = 0;
+  for (int64_t c = 0; c < blocks; c += 1024) {
+    const int64_t i = c + threadIdx.x;
+    const int32_t v = i < blocks ? a.heads[i] : 0;
+    int64_t all;
+    const int64_t before = block_excl_scan<1024>(v, &all);
+    if (i < blocks) a.heads[i] = (int32_t)(carry + before);
+    carry += all;
+  }
+  if (threadIdx.x == 0) *count = carry;
+}
+
+__global__ __launch_bounds__(ST) void k_heads_rank(IdSort a, const int32_t *key,
+                                                   int32_t *node_out) {
+  // a thread takes HEADS / ST entries in a row
+  constexpr int PER = HEADS / ST;
+  const int64_t i0 = (int64_t)blockIdx.x * HEADS + threadIdx.x * PER;
+  bool head[PER];
+  int mine = 0;
+#pragma unroll
+  for (int r = 0; r < PER; ++r) mine += head[r] = is_head(key, i0 + r, a.n, a.slots);
+  int64_t all;
+  int64_t at = a.heads[blockIdx.x] + block_excl_scan<ST>(mine, &all) - 1;
+#pragma unroll
+  for (int r = 0; r < PER; ++r) {
+    const int64_t i = i0 + r;
+    if (i >= a.n) break;
+    at += head[r];
+    const int32_t k = key[i];
+    a.dst[i] = k < a.slots ? (int32_t)at : -1;
+    if (head[r]) node_out[at] = k;
+  }
+}
+
+// ------------------------------------------------------------------ short lists
+// One block: keys and places as 64-bit numbers, sorted by exchanges in shared memory.
+constexpr int SMALL_T = 1024;
+__global__ __launch_bounds__(SMALL_T) void k_sort_small(IdSort a, int32_t *node_out,
+                                                        int64_t *count, int32_t *status) {
+  __shared__ uint64_t s[SMALL];
+  const int n = (int)a.n;
+  int size = 2;
+  while (size < n) size <<= 1;
+  bool bad = false;
+  for (int i = threadIdx.x; i < size; i += SMALL_T) {
+    const int32_t k = i < n ? sort_key(a.ids[i], a.slots, &bad) : -1;
+    s[i] = i < n ? (uint64_t)(uint32_t)k << 32 | (uint32_t)i : ~0ull;
+    if (!a.compact && i < n && k < a.slots) a.seen[k] = 1;
+  }
+  if (bad && status) atomicOr(status, 1);
+  if (threadIdx.x == 0) *a.n_long = 0;
+  for (int run = 2; run <= size; run <<= 1) {
+    for (int step = run >> 1; step > 0; step >>= 1) {
+      __syncthreads();
+      const int t = threadIdx.x;
+      if (t < size / 2) {
+        const int i = 2 * t - (t & (step - 1)), j = i + step;
+        const uint64_t x = s[i], y = s[j];
+        if ((x > y) == ((i & run) == 0)) {
+          s[i] = y;
+          s[j] = x;
+        }
+      }
+    }
+  }
+  __syncthreads();
+  // SMALL / SMALL_T entries in a row per thread
+  constexpr int PER = SMALL / SMALL_T;
+  bool head[PER];
+  int mine = 0;
+#pragma unroll
+  for (int r = 0; r < PER; ++r) {
+    const int i = threadIdx.x * PER + r;
+    const int32_t k = i < n ? (int32_t)(s[i] >> 32) : -1;
+    head[r] = i < n && k < a.slots && (i == 0 || (int32_t)(s[i - 1] >> 32) != k);
+    mine += head[r];
+  }
+  int64_t all = 0;
+  int64_t at = block_excl_scan<SMALL_T>(mine, &all) - 1;
+  if (a.compact && threadIdx.x == 0) *count = all;
+#pragma unroll
+  for (int r = 0; r < PER; ++r) {
+    const int i = threadIdx.x * PER + r;
+    if (i >= n) break;
+    const int32_t k = (int32_t)(s[i] >> 32);
+    at += head[r];
+    a.order[i] = (int32_t)(uint32_t)s[i];
+    a.dst[i] = !a.compact ? k : k < a.slots ? (int32_t)at : -1;
+    if (a.compact && head[r]) node_out[at] = k;
+  }
+}
+
+}  // namespace
+
+// Entries of a chunk: shorter ones until their groups of lanes fill the chip.
+static int chunk_len(int64_t n) { return n >= (1 << 20) ? 64 : n >= (1 << 17) ? 32 : 16; }
+
+void carve_sort(IdSort &a, Carve &c) {
+  const int64_t n = a.n;
+  a.C = chunk_len(n);
+  a.chunks = (n + a.C - 1) / a.C;
+  const int64_t tiles = (n + ST * sort_rounds(n) - 1) / (ST * sort_rounds(n));
+  for (int i = 0; i < 2; ++i) {
+    a.key[i] = c.take<int32_t>((size_t)n);
+    a.pos[i] = c.take<int32_t>((size_t)n);
+  }
+  a.dst = a.key[0];
+  a.order = a.pos[0];
+  if (a.compact) a.dst = c.take<int32_t>((size_t)n);
+  a.seen = a.compact ? nullptr : c.take<uint8_t>((size_t)a.slots);
+  a.cnt = c.take<uint32_t>((size_t)BINS * (size_t)tiles);
+  a.tot = c.take<uint32_t>(BINS);
+  a.heads = a.compact ? c.take<int32_t>((size_t)((n + HEADS - 1) / HEADS)) : nullptr;
+  a.n_long = c.take<int32_t>(1);
+  a.long_at = c.take<int32_t>((size_t)a.chunks + 1);
+  a.part = n > 2 * a.C ? c.take<float>((size_t)(2 * a.chunks * a.width)) : nullptr;
+}
+
+size_t sort_room(IdSort a) {
+  size_t most = 0;
+  const int64_t n = a.n;
+  for (int64_t len : {n, (int64_t)(1 << 20), (int64_t)(1 << 20) - 1, (int64_t)(1 << 17) - 1}) {
+    if (len > n) continue;
+    a.n = len;
+    Carve c(nullptr);
+    carve_sort(a, c);
+    if (c.used > most) most = c.used;
+  }
+  return most;
+}
+
+int run_sort(IdSort &a, int32_t *node_out, int64_t *count, int32_t *status, hipStream_t s) {
+  if (!a.compact) {
+    // (carved in pieces of 256 bytes, so whole words hold it)
+    DG_TRY(fill_u64((uint64_t *)a.seen, (size_t)(a.slots + 7) / 8, 0, s));
+  }
+  if (a.n == 0) return a.compact ? fill_u64((uint64_t *)count, 1, 0, s) : DG_OK;
+  if (a.n <= SMALL) {
+    hipLaunchKernelGGL(k_sort_small, dim3(1), dim3(SMALL_T), 0, s, a, node_out, count, status);
+    DG_HIP(hipGetLastError());
+    return DG_OK;
+  }
+  const int total = log2_up(a.slots + 1);  // bits of the keys 0..slots
+  const int passes = total <= MAX_BITS ? 1 : (total + MAX_BITS - 1) / MAX_BITS;
+  const int each = (total + passes - 1) / passes;
+  const int rounds = sort_rounds(a.n);
+  Pass p;
+  p.tiles = (a.n + ST * rounds - 1) / (ST * rounds);
+  for (int i = 0; i < passes; ++i) {
+    const int in = (i + 1) & 1, out = i & 1;
+    p.key = i ? a.key[in] : a.ids;
+    p.pos = i ? a.pos[in] : nullptr;
+    p.key_out = a.key[out];
+    p.pos_out = a.pos[out];
+    p.shift = i * each;
+    p.bits = total - p.shift < each ? total - p.shift : each;
+    const dim3 g((unsigned)p.tiles), b(ST);
+    const int bins = 1 << p.bits;
+    auto go = [&](auto r, auto first) {
+      constexpr int R = decltype(r)::value;
+      constexpr bool F = decltype(first)::value;
+      hipLaunchKernelGGL((k_sort_count<R, F>), g, b, 0, s, a, p, status);
+      hipLaunchKernelGGL(k_sort_scan, dim3((bins + SW - 1) / SW), b, 0, s, a, p.tiles, bins);
+      hipLaunchKernelGGL((k_sort_place<R, F>), g, b, 0, s, a, p);
+    };
+    using std::integral_constant;
+    if (rounds == 16) {
+      if (i == 0) go(integral_constant<int, 16>(), std::true_type());
+      else go(integral_constant<int, 16>(), std::false_type());
+    } else {
+      if (i == 0) go(integral_constant<int, 4>(), std::true_type());
+      else go(integral_constant<int, 4>(), std::false_type());
+    }
+  }
+  const int last = (passes - 1) & 1;
+  a.order = a.pos[last];
+  if (a.compact) {
+    const int64_t blocks = (a.n + HEADS - 1) / HEADS;
+    hipLaunchKernelGGL(k_heads_count, dim3((unsigned)blocks), dim3(ST), 0, s, a, a.key[last]);
+    hipLaunchKernelGGL(k_heads_scan, dim3(1), dim3(1024), 0, s, a, blocks, count);
+    hipLaunchKernelGGL(k_heads_rank, dim3((unsigned)blocks), dim3(ST), 0, s, a, a.key[last],
+                       node_out);
+  } else {
+    a.dst = a.key[last];
+  }
+  DG_HIP(hipGetLastError());
+  return DG_OK;
+}
+
+}  // namespace dg

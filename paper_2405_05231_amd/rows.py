@@ -1,0 +1,336 @@
+"""Operators on a model's rows: embedding rows, RMS norm and neighbour attention, each
+with its gradient (the "Model rows" of include/dg.h).
+
+As in the rest of the package, these functions marshal torch tensors into the C ABI and
+the work runs in the library's kernels, asynchronously on the given stream (by default
+the current one).  Results, workspaces and temporaries are made on that stream.  `status`
+is an optional int32 tensor of one element into which the kernels OR 1 for an index out
+of range and 2 for offsets out of order; such entries add nothing.
+"""
+from __future__ import annotations
+
+import contextlib
+from dataclasses import dataclass
+
+import torch
+
+from . import _lib
+from ._lib import check, load
+
+_L = load()
+
+_TYPES = {torch.float32: _lib.DG_F32, torch.float16: _lib.DG_F16, torch.bfloat16: _lib.DG_BF16,
+          torch.float8_e4m3fn: _lib.DG_F8E4M3}
+_WIDE = (torch.float32, torch.float16, torch.bfloat16)
+
+
+def _on(stream):
+    """(context that makes allocations on the stream, its handle)."""
+    if stream is None:
+        return contextlib.nullcontext(), torch.cuda.current_stream().cuda_stream
+    return torch.cuda.stream(stream), stream.cuda_stream
+
+
+def _gpu(t, name: str, dtypes, device=None):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name}: expected {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must live in GPU memory")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: expected device {device}, got {t.device}")
+
+
+def _whole(t, name: str, dtype, device, numel=None):
+    _gpu(t, name, (dtype,), device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"{name}: expected {numel} elements, got {t.numel()}")
+
+
+def _rows(t, name: str, dtypes, device=None, shape=None, dims: int = 2) -> int:
+    """Checks a tensor of rows (the elements of a row adjacent, rows apart by any stride)
+    and returns the stride of its rows."""
+    _gpu(t, name, dtypes, device)
+    if t.dim() != dims:
+        raise ValueError(f"{name}: expected {dims} dimensions, got {t.dim()}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    width = 1
+    for d in range(dims - 1, 0, -1):
+        if t.shape[d] != 1 and t.stride(d) != width:
+            raise ValueError(f"{name}: the elements of a row must be adjacent")
+        width *= t.shape[d]
+    if t.shape[0] <= 1:
+        return max(width, 1)
+    if t.stride(0) < width:
+        raise ValueError(f"{name}: rows must not overlap")
+    return t.stride(0)
+
+
+def _out(t, name: str, shape, dtype, device):
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _whole(t, name, dtype, device)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _status(t, device):
+    if t is not None:
+        _whole(t, "status", torch.int32, device, 1)
+    return _ptr(t)
+
+
+def _workspace(nbytes: int, device, ws):
+    if ws is not None:
+        if not (isinstance(ws, torch.Tensor) and ws.device == device and ws.is_contiguous()):
+            raise ValueError("workspace: expected a contiguous tensor on the inputs' device")
+        if ws.numel() * ws.element_size() >= nbytes:
+            return ws, ws.numel() * ws.element_size()
+    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device), max(nbytes, 256)
+
+
+# ------------------------------------------------------------------------ embedding rows
+def embed_rows(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
+               row_scale: torch.Tensor | None = None, dtype: torch.dtype | None = None,
+               out: torch.Tensor | None = None, status: torch.Tensor | None = None,
+               stream=None) -> torch.Tensor:
+    """Rows of a learned table (dg_embed_rows): out[i] = scale * row_scale[ids[i]] *
+    table[ids[i]].  table: [N, D] in float32, float16, bfloat16 or float8_e4m3fn; ids:
+    int32 [n], -1 for a zero row; row_scale: float32 [N], for tables in 8 bits.  dtype:
+    the result's (by default the table's, float32 for a table in 8 bits)."""
+    stride = _rows(table, "table", tuple(_TYPES))
+    dev = table.device
+    _whole(ids, "ids", torch.int32, dev)
+    N, D = table.shape
+    if row_scale is not None:
+        _whole(row_scale, "row_scale", torch.float32, dev, N)
+    if dtype is None:
+        dtype = out.dtype if out is not None else (
+            table.dtype if table.dtype in _WIDE else torch.float32)
+    if dtype not in _WIDE:
+        raise TypeError(f"dtype: expected float32, float16 or bfloat16, got {dtype}")
+    n = ids.numel()
+    on, s = _on(stream)
+    with on:
+        if out is None:
+            out = torch.empty((n, D), dtype=dtype, device=dev)
+        out_stride = _rows(out, "out", (dtype,), dev, (n, D))
+        check(_L.dg_embed_rows(_ptr(table), _TYPES[table.dtype], N, D, stride, _ptr(row_scale),
+                               _ptr(ids), n, scale, _ptr(out), _TYPES[dtype], out_stride,
+                               _status(status, dev), s))
+    return out
+
+
+def embed_rows_grad(grad_out: torch.Tensor, ids: torch.Tensor, num_rows: int, scale: float = 1.0,
+                    sparse: bool = False, dtype: torch.dtype | None = None,
+                    out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                    status: torch.Tensor | None = None, stream=None):
+    """Gradient of embed_rows towards a table of num_rows rows (dg_embed_rows_grad): for
+    each node the sum of scale * grad_out over the list entries that hold it, in list
+    order.  Returns the whole gradient [num_rows, D], or with sparse=True (nodes int32
+    [u], ascending, sums [u, D]), which waits for the number of nodes u.  dtype: the
+    result's, by default grad_out's."""
+    stride = _rows(grad_out, "grad_out", _WIDE)
+    dev = grad_out.device
+    n, D = grad_out.shape
+    _whole(ids, "ids", torch.int32, dev, n)
+    if dtype is None:
+        dtype = out.dtype if out is not None else grad_out.dtype
+    if dtype not in _WIDE:
+        raise TypeError(f"dtype: expected float32, float16 or bfloat16, got {dtype}")
+    most = min(n, num_rows) if sparse else num_rows
+    on, s = _on(stream)
+    with on:
+        grad = _out(out, "out", (most, D), dtype, dev)
+        nodes = count = None
+        if sparse:
+            nodes = torch.empty(max(most, 1), dtype=torch.int32, device=dev)
+            count = torch.empty(1, dtype=torch.int64, device=dev)
+        ws, ws_bytes = _workspace(
+            _L.dg_embed_rows_grad_workspace_bytes(num_rows, D, n, int(sparse)), dev, workspace)
+        check(_L.dg_embed_rows_grad(_ptr(grad_out), _TYPES[grad_out.dtype], stride, _ptr(ids), n,
+                                    num_rows, D, scale, _ptr(grad), _TYPES[dtype], _ptr(nodes),
+                                    _ptr(count), _status(status, dev), _ptr(ws), ws_bytes, s))
+        if not sparse:
+            return grad
+        u = int(count)
+        return nodes[:u], grad[:u]
+
+
+# ------------------------------------------------------------------------ RMS norm
+@dataclass
+class NormResult:
+    y: torch.Tensor             # [n, D] in the rows' type, or float8_e4m3fn codes
+    scale: torch.Tensor | None  # float32 [n, groups]: y ~ code * scale (8 bits only)
+    h: torch.Tensor             # [n, D] x + residual (x itself without a residual)
+    rstd: torch.Tensor          # float32 [n]
+
+
+def norm_rows(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | None = None,
+              eps: float = 1e-6, dtype: torch.dtype | None = None, group: int = 0,
+              stream=None) -> NormResult:
+    """RMS norm of the rows of x + residual, times weight (dg_norm_rows).  dtype: the
+    type of y, x's own (by default) or float8_e4m3fn, with one scale per row (group = 0)
+    or per group of 32, 64 or 128 columns."""
+    stride = _rows(x, "x", _WIDE)
+    dev = x.device
+    n, D = x.shape
+    _whole(weight, "weight", torch.float32, dev, D)
+    res_stride = 0
+    if residual is not None:
+        res_stride = _rows(residual, "residual", (x.dtype,), dev, (n, D))
+    if dtype is None:
+        dtype = x.dtype
+    if dtype not in _TYPES:
+        raise TypeError(f"dtype: expected {x.dtype} or torch.float8_e4m3fn, got {dtype}")
+    on, s = _on(stream)
+    with on:
+        y = torch.empty((n, D), dtype=dtype, device=dev)
+        rstd = torch.empty(n, dtype=torch.float32, device=dev)
+        h = torch.empty((n, D), dtype=x.dtype, device=dev) if residual is not None else None
+        scales = None
+        if dtype == torch.float8_e4m3fn:
+            groups = -(-D // group) if group > 0 else 1
+            scales = torch.empty((n, groups), dtype=torch.float32, device=dev)
+        check(_L.dg_norm_rows(_ptr(x), stride, _ptr(residual), res_stride, _TYPES[x.dtype], n, D,
+                              _ptr(weight), eps, _ptr(y), _TYPES[dtype], group, _ptr(scales),
+                              _ptr(h), _ptr(rstd), s))
+    return NormResult(y, scales, x if h is None else h, rstd)
+
+
+def norm_rows_grad(grad_y: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, weight: torch.Tensor,
+                   grad_h: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                   stream=None):
+    """Gradient of norm_rows (dg_norm_rows_grad), from its h and rstd: (grad_x [n, D], which
+    is the residual's gradient too, grad_weight float32 [D]).  grad_h: the gradient that
+    reaches h by itself.  An 8-bit y counts as y before its rounding."""
+    stride = _rows(grad_y, "grad_y", _WIDE)
+    dev = grad_y.device
+    n, D = grad_y.shape
+    h_stride = _rows(h, "h", (grad_y.dtype,), dev, (n, D))
+    _whole(rstd, "rstd", torch.float32, dev, n)
+    _whole(weight, "weight", torch.float32, dev, D)
+    gh_stride = 0
+    if grad_h is not None:
+        gh_stride = _rows(grad_h, "grad_h", (grad_y.dtype,), dev, (n, D))
+    on, s = _on(stream)
+    with on:
+        gx = torch.empty((n, D), dtype=grad_y.dtype, device=dev)
+        gw = torch.empty(D, dtype=torch.float32, device=dev)
+        ws, ws_bytes = _workspace(_L.dg_norm_rows_grad_workspace_bytes(n, D), dev, workspace)
+        check(_L.dg_norm_rows_grad(_ptr(grad_y), stride, _ptr(h), h_stride, _ptr(rstd),
+                                   _ptr(weight), _ptr(grad_h), gh_stride, _TYPES[grad_y.dtype], n,
+                                   D, _ptr(gx), _ptr(gw), _ptr(ws), ws_bytes, s))
+    return gx, gw
+
+
+# ------------------------------------------------------------------------ neighbour attention
+@dataclass
+class AttendResult:
+    out: torch.Tensor  # [nq, heads, D]
+    lse: torch.Tensor  # float32 [nq, heads]; -inf for a row without a neighbour
+
+
+@dataclass
+class AttendGrads:
+    q: torch.Tensor
+    k: torch.Tensor
+    v: torch.Tensor
+    bias: torch.Tensor | None
+
+
+def edge_offsets(edge_src: torch.Tensor, num_rows: int, out: torch.Tensor | None = None,
+                 status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Offsets int64 [num_rows + 1] of an edge list sorted by row (dg_edge_offsets), as
+    sample_group lists a mini-batch's edges by edge_src."""
+    dev = edge_src.device if isinstance(edge_src, torch.Tensor) else None
+    _whole(edge_src, "edge_src", torch.int32, dev)
+    on, s = _on(stream)
+    with on:
+        out = _out(out, "out", (num_rows + 1,), torch.int64, dev)
+        check(_L.dg_edge_offsets(_ptr(edge_src), edge_src.numel(), num_rows, _ptr(out),
+                                 _status(status, dev), s))
+    return out
+
+
+def _attend_args(q, k, v, offsets, indices, bias):
+    qs = _rows(q, "q", _WIDE, dims=3)
+    dev, dt = q.device, (q.dtype,)
+    nq, heads, D = q.shape
+    ks = _rows(k, "k", dt, dev, dims=3)
+    nkv, kv_heads = k.shape[:2]
+    if k.shape[2] != D:
+        raise ValueError(f"k: expected heads of {D} elements, got {k.shape[2]}")
+    vs = _rows(v, "v", dt, dev, tuple(k.shape), dims=3)
+    _whole(offsets, "offsets", torch.int64, dev, nq + 1)
+    _whole(indices, "indices", torch.int32, dev)
+    edges, bias_heads = indices.numel(), 0
+    if bias is not None:
+        _whole(bias, "bias", torch.float32, dev)
+        bias_heads = 1 if bias.dim() == 1 else heads
+        if tuple(bias.shape) not in ((edges,), (edges, heads)):
+            raise ValueError(f"bias: expected shape ({edges},) or ({edges}, {heads}), "
+                             f"got {tuple(bias.shape)}")
+    return dev, qs, ks, vs, nq, nkv, heads, kv_heads, D, edges, bias_heads
+
+
+def attend_edges(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor,
+                 indices: torch.Tensor, scale: float | None = None,
+                 bias: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                 status: torch.Tensor | None = None, stream=None) -> AttendResult:
+    """Attention of rows over lists of neighbours (dg_attend_edges): row i of q [nq, heads,
+    D] attends over rows indices[offsets[i]:offsets[i + 1]] of k and v [nkv, kv_heads, D];
+    heads is a multiple of kv_heads.  offsets int64 [nq + 1], indices int32 [edges] (-1: no
+    neighbour); bias: float32 [edges] or [edges, heads], added to the scores, -inf for a
+    masked edge.  scale: 1/sqrt(D) by default."""
+    dev, qs, ks, vs, nq, nkv, heads, kv_heads, D, edges, bias_heads = _attend_args(
+        q, k, v, offsets, indices, bias)
+    on, s = _on(stream)
+    with on:
+        out = torch.empty((nq, heads, D), dtype=q.dtype, device=dev)
+        lse = torch.empty((nq, heads), dtype=torch.float32, device=dev)
+        ws, ws_bytes = _workspace(_L.dg_attend_edges_workspace_bytes(edges, heads, D), dev,
+                                  workspace)
+        check(_L.dg_attend_edges(_ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _TYPES[q.dtype], nq, nkv,
+                                 heads, kv_heads, D, _ptr(offsets), _ptr(indices), edges,
+                                 _ptr(bias), bias_heads, D ** -0.5 if scale is None else scale,
+                                 _ptr(out), _ptr(lse), _status(status, dev), _ptr(ws), ws_bytes,
+                                 s))
+    return AttendResult(out, lse)
+
+
+def attend_edges_grad(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                      out: torch.Tensor, lse: torch.Tensor, offsets: torch.Tensor,
+                      indices: torch.Tensor, scale: float | None = None,
+                      bias: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                      status: torch.Tensor | None = None, stream=None) -> AttendGrads:
+    """Gradient of attend_edges (dg_attend_edges_grad) from its results out and lse; the
+    probabilities are recomputed.  Sums over shared keys run in a fixed order."""
+    dev, qs, ks, vs, nq, nkv, heads, kv_heads, D, edges, bias_heads = _attend_args(
+        q, k, v, offsets, indices, bias)
+    gs = _rows(grad_out, "grad_out", (q.dtype,), dev, tuple(q.shape), dims=3)
+    os_ = _rows(out, "out", (q.dtype,), dev, tuple(q.shape), dims=3)
+    _whole(lse, "lse", torch.float32, dev, nq * heads)
+    on, s = _on(stream)
+    with on:
+        gq = torch.empty((nq, heads, D), dtype=q.dtype, device=dev)
+        gk = torch.empty((nkv, kv_heads, D), dtype=q.dtype, device=dev)
+        gv = torch.empty((nkv, kv_heads, D), dtype=q.dtype, device=dev)
+        gb = torch.empty(bias.shape, dtype=torch.float32, device=dev) if bias is not None else None
+        ws, ws_bytes = _workspace(
+            _L.dg_attend_edges_grad_workspace_bytes(edges, nkv, heads, kv_heads, D), dev, workspace)
+        check(_L.dg_attend_edges_grad(
+            _ptr(grad_out), gs, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(out), os_, _ptr(lse),
+            _TYPES[q.dtype], nq, nkv, heads, kv_heads, D, _ptr(offsets), _ptr(indices), edges,
+            _ptr(bias), bias_heads, D ** -0.5 if scale is None else scale, _ptr(gq), _ptr(gk),
+            _ptr(gv), _ptr(gb), _status(status, dev), _ptr(ws), ws_bytes, s))
+    return AttendGrads(gq, gk, gv, gb)

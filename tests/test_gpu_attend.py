@@ -1,0 +1,536 @@
+"""Neighbour attention and its gradient against the formulas in 64 bits.
+
+Tolerances are bounds on what 32-bit arithmetic may do, from the inputs.  With u = 2^-24, a
+score is off by at most es = (D + 4) u (scale sum|q k| + |b|); a probability, by e^x - 1 of
+its score's, its row's lse's and the exponential's error, taken as ep = 2 (2 max es + 4 u
+(max|s| + |lse|) + 16 u) of its value; sums of k terms add (k + 4) u of the sum of
+magnitudes; a result's rounding to its type half a unit of its value (2^-24, 2^-11, 2^-8;
+2^-25 at least for the smallest 16-bit numbers).  Each test passes its magnitudes through
+the same sums as the values."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+U = 2.0 ** -24
+HALF_UNIT = {torch.float32: U, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+WIDE = list(HALF_UNIT)
+NINF = float("-inf")
+
+
+@pytest.fixture(scope="module")
+def dg():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2405_05231_amd as m
+    return m
+
+
+def rng(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def randn(seed, *shape, dtype=torch.float32):
+    return torch.randn(*shape, device=DEV, generator=rng(seed)).to(dtype)
+
+
+def offsets_of(lens):
+    lens = torch.as_tensor(lens, dtype=torch.int64, device=DEV)
+    return torch.cat([lens.new_zeros(1), lens.cumsum(0)])
+
+
+def problem(lens, nkv, heads, kv_heads, D, dtype, bias=None, seed=0):
+    off = offsets_of(lens)
+    nq, E = off.numel() - 1, int(off[-1])
+    p = dict(q=randn(seed + 1, nq, heads, D, dtype=dtype),
+             k=randn(seed + 2, nkv, kv_heads, D, dtype=dtype),
+             v=randn(seed + 3, nkv, kv_heads, D, dtype=dtype), offsets=off,
+             indices=torch.randint(0, nkv, (E,), device=DEV, dtype=torch.int32,
+                                   generator=rng(seed + 4)), bias=None, scale=D ** -0.5)
+    if bias:
+        b = randn(seed + 5, *((E,) if bias == "edge" else (E, heads)))
+        p["bias"] = torch.where(torch.rand(b.shape, device=DEV, generator=rng(seed + 6)) < 0.1,
+                                NINF, b)
+    return p
+
+
+def parts(p):
+    """Everything of the forward pass in 64 bits, per edge and head; edges of index -1 and
+    masked ones have weight 0."""
+    q, k, v = (p[n].double() for n in "qkv")
+    nq, heads, D = q.shape
+    off = p["offsets"]
+    row = torch.repeat_interleave(torch.arange(nq, device=DEV), off.diff())
+    none = (p["indices"] < 0) | (p["indices"] >= k.shape[0])
+    at = torch.where(none, 0, p["indices"]).long()
+    share = heads // k.shape[1]
+    kk, vv = k.repeat_interleave(share, 1)[at], v.repeat_interleave(share, 1)[at]
+    s = (q[row] * kk).sum(2) * p["scale"]
+    es = (q[row] * kk).abs().sum(2) * abs(p["scale"])
+    masked = none[:, None].expand_as(s)
+    if p["bias"] is not None:
+        b = p["bias"].double()
+        b = b[:, None].expand_as(s) if b.dim() == 1 else b
+        masked = masked | (b == NINF)
+        s, es = s + b, es + b.abs()
+    s = torch.where(masked, NINF, s)
+    es = torch.where(masked, 0.0, es) * (D + 4) * U
+    kk, vv = (torch.where(masked[:, :, None], 0.0, x) for x in (kk, vv))
+    return row, at, kk, vv, s, es, nq, heads
+
+
+def by_row(row, n, x, how="sum"):
+    out = torch.zeros((n, *x.shape[1:]), dtype=x.dtype, device=DEV)
+    if how == "max":
+        out.fill_(NINF)
+        idx = row.view(-1, *[1] * (x.dim() - 1)).expand_as(x)
+        return out.scatter_reduce_(0, idx, x, "amax")
+    # differences of running sums in the order of the rows (2^-53 of them: far below all bounds)
+    rows, order = row.sort(stable=True)
+    ends = torch.searchsorted(rows, torch.arange(n + 1, device=DEV))
+    sums = torch.cat([torch.zeros_like(x[:1]), x[order].cumsum(0)]) if x.numel() else x
+    return sums[ends[1:]] - sums[ends[:-1]] if x.numel() else out
+
+
+def reference(p):
+    row, at, kk, vv, s, es, nq, heads = parts(p)
+    top = by_row(row, nq, s, "max")
+    safe = torch.where(top == NINF, 0.0, top)
+    w = torch.exp(s - safe[row])
+    total = by_row(row, nq, w)
+    lse = torch.where(total > 0, safe + total.log(), NINF)
+    pr = w / torch.where(total > 0, total, 1.0)[row]
+    out = by_row(row, nq, pr[:, :, None] * vv)
+    mag = by_row(row, nq, pr[:, :, None] * vv.abs())
+    live = torch.where(s == NINF, 0.0, s.abs())
+    most = by_row(row, nq, live, "max").clamp_min(0)
+    err = by_row(row, nq, es, "max").clamp_min(0)
+    ep = 2 * (2 * err + 4 * U * (most + torch.where(lse == NINF, 0.0, lse.abs())) + 16 * U)
+    return out, lse, mag, ep
+
+
+def close(got, want, tol):
+    assert got.shape == want.shape
+    same = (got.double() == want) | (got.double() - want).abs().le(tol)
+    assert same.all(), (got[~same][:4], want[~same][:4], tol[~same][:4])
+
+
+def check_forward(dg, p, **kw):
+    r = dg.attend_edges(p["q"], p["k"], p["v"], p["offsets"], p["indices"], scale=p["scale"],
+                        bias=p["bias"], **kw)
+    out, lse, mag, ep = reference(p)
+    k = p["offsets"].diff().double()[:, None] + 4
+    unit = HALF_UNIT[p["q"].dtype]
+    tol = (ep + 2 * k * U)[:, :, None] * mag
+    close(r.out, out, tol + unit * (out.abs() + tol) + 2.0 ** -25)
+    close(r.lse, lse, ep + k * U)
+    return r
+
+
+def check_gradient(dg, p, r=None, **kw):
+    if r is None:
+        r = dg.attend_edges(p["q"], p["k"], p["v"], p["offsets"], p["indices"], scale=p["scale"],
+                            bias=p["bias"])
+    go = randn(77, *p["q"].shape, dtype=p["q"].dtype)
+    g = dg.attend_edges_grad(go, p["q"], p["k"], p["v"], r.out, r.lse, p["offsets"], p["indices"],
+                             scale=p["scale"], bias=p["bias"], **kw)
+    row, at, kk, vv, s, es, nq, heads = parts(p)
+    unit = HALF_UNIT[p["q"].dtype]
+    D, nkv, kv_heads = p["q"].shape[2], p["k"].shape[0], p["k"].shape[1]
+    lse = r.lse.double()
+    some = lse != NINF
+    lse = torch.where(some, lse, 0.0)
+    pr = torch.where(some[row], torch.exp(s - lse[row]), 0.0)
+    live = torch.where(s == NINF, 0.0, s.abs())
+    ep = 2 * (es + 4 * U * (live + lse[row].abs()) + 16 * U)
+    gd, od = go.double(), r.out.double()
+    dp, delta = (gd[row] * vv).sum(2), (gd * od).sum(2)
+    edp = (D + 4) * U * ((gd[row] * vv).abs().sum(2) + (gd * od).abs().sum(2)[row])
+    ds = pr * (dp - delta[row])
+    eds = pr * (edp + (ep + 2 * U) * (dp - delta[row]).abs())
+    # an edge in the sorted order of its key and a row's own list
+    k_row = p["offsets"].diff().double()[:, None, None] + 4
+    k_key = torch.bincount(at, minlength=nkv).double()[:, None, None] * (heads // kv_heads) + 4
+
+    def to_keys(x):
+        return by_row(at, nkv, x.view(-1, kv_heads, heads // kv_heads, D).sum(2))
+
+    a = abs(p["scale"])
+    qd = p["q"].double()[row]
+    gone = (p["indices"] < 0) | (p["indices"] >= nkv)
+    live_e = torch.where(gone, 0.0, 1.0)[:, None, None]
+    for got, add, count, val, wgt, ewgt, rows in (
+            (g.q, lambda x: by_row(row, nq, x), k_row, a, ds, eds, kk),
+            (g.k, to_keys, k_key, a, ds, eds, qd), (g.v, to_keys, k_key, 1.0, pr, pr * ep, gd[row])):
+        want = add(live_e * wgt[:, :, None] * rows) * val
+        tol = add(live_e * (ewgt[:, :, None]) * rows.abs()) * val
+        tol = tol + count * U * add(live_e * (wgt.abs() + ewgt)[:, :, None] * rows.abs()) * val
+        close(got, want, tol + unit * (want.abs() + tol) + 2.0 ** -25)
+    if p["bias"] is None:
+        assert g.bias is None
+    elif p["bias"].dim() == 2:
+        close(g.bias, ds, eds + U * ds.abs() + 1e-30)
+    else:
+        close(g.bias, ds.sum(1), eds.sum(1) + heads * U * ds.abs().sum(1) + 1e-30)
+    return g
+
+
+LENS = [0, 1, 2, 3, 4, 5, 7, 8, 9, 0, 15, 16, 17, 33, 70, 1, 0]
+
+
+@pytest.mark.parametrize("dtype", WIDE)
+@pytest.mark.parametrize("heads,kv_heads,D", [
+    (1, 1, 1), (1, 1, 3), (2, 2, 7), (1, 1, 8), (3, 3, 16), (4, 4, 32), (6, 2, 50), (8, 8, 32),
+    (8, 1, 64), (4, 2, 96), (5, 5, 128), (2, 1, 200), (16, 16, 24), (12, 3, 256), (20, 20, 40)])
+@pytest.mark.parametrize("bias", [None, "edge", "head"])
+def test_attention(dg, dtype, heads, kv_heads, D, bias):
+    p = problem(LENS, 40, heads, kv_heads, D, dtype, bias)
+    check_gradient(dg, p, check_forward(dg, p))
+
+
+@pytest.mark.parametrize("lens", [
+    [0], [1], [0, 0, 0], [127], [128], [129], [130, 0, 1], [255, 257], [1, 300, 2, 400, 0],
+    [5000], [128] * 9, [129] * 9, [64, 1000, 64, 1000], [3] * 1000 + [2000] + [4] * 777,
+    [0] * 500 + [700] + [0] * 500, [300_001], [9] * 3000 + [270_000] + [1] * 99])
+@pytest.mark.parametrize("bias", [None, "edge"])
+def test_lists_of_every_length(dg, lens, bias):
+    """Lists on both sides of the chunk length (128 edges here, 256 from 2^18 edges on), that
+    start and end on and off its multiples, alone and among short ones."""
+    p = problem(lens, 333, 4, 2, 16, torch.float32, bias, seed=len(lens))
+    check_gradient(dg, p, check_forward(dg, p))
+
+
+@pytest.mark.parametrize("E", [2047, 2048, 2049, 140_000, 1_100_000])
+@pytest.mark.parametrize("nkv", [1, 7, 50_000])
+def test_keys_with_many_and_without_edges(dg, E, nkv):
+    lens = [5] * (E // 5) + [E % 5]
+    p = problem(lens, nkv, 2, 2, 8, torch.float32, seed=E)
+    if nkv > 100:  # most edges meet few keys, most keys no edge
+        p["indices"] = (torch.rand(E, device=DEV, generator=rng(E)).pow(8) * nkv).int()
+    check_gradient(dg, p, check_forward(dg, p))
+
+
+def test_one_row_and_all_of_a_graphs_lists(dg):
+    """Serving: one query against a long list, and a CSR graph's own arrays as the lists."""
+    check_forward(dg, problem([100_003], 100_003, 8, 2, 64, torch.bfloat16))
+    import synth
+    w = synth.make_workload("T")
+    off, idx = w.offsets.to(DEV), w.indices.to(DEV)
+    n = off.numel() - 1
+    p = dict(q=randn(1, n, 2, 16), k=randn(2, n, 2, 16), v=randn(3, n, 2, 16), offsets=off,
+             indices=idx, bias=None, scale=0.25)
+    check_gradient(dg, p, check_forward(dg, p))
+
+
+@pytest.mark.parametrize("dtype", WIDE)
+def test_strided_and_unaligned_rows(dg, dtype):
+    """q, k and v as slices of one product's rows, at odd offsets."""
+    lens, heads, D = [3, 0, 9, 200, 5], 3, 20
+    p = problem(lens, 5, heads, heads, D, dtype, "edge")
+    wide = torch.zeros(5, 3 * heads * D + 7, dtype=dtype, device=DEV)
+    for i, n in enumerate("qkv"):
+        part = wide[:, 3 + i * heads * D:3 + (i + 1) * heads * D]
+        part.copy_(p[n].reshape(5, -1))
+        p[n] = part.view(5, heads, D)
+    check_gradient(dg, p, check_forward(dg, p))
+
+
+@pytest.mark.parametrize("lens", [[4, 3, 0, 6], [400, 3, 0, 300]])
+def test_rows_that_a_mask_empties(dg, lens):
+    p = problem(lens, 30, 4, 4, 12, torch.float32, "edge")
+    off = p["offsets"].tolist()
+    p["bias"][off[0]:off[1]] = NINF  # all of row 0
+    p["bias"][off[3]:off[4] - 1] = NINF  # all but one of row 3
+    p["bias"][off[4] - 1] = 0.5
+    r = check_forward(dg, p)
+    assert not r.out[0].any() and (r.lse[0] == NINF).all()
+    assert not r.out[2].any() and (r.lse[2] == NINF).all()
+    g = check_gradient(dg, p, r)
+    assert not g.q[0].any() and not g.q[2].any() and not g.bias[off[0]:off[1]].any()
+
+
+@pytest.mark.parametrize("dtype", WIDE)
+@pytest.mark.parametrize("D", [5, 16])
+@pytest.mark.parametrize("lens", [[6, 4, 9], [600, 4, 9]])
+def test_masked_places_may_hold_anything(dg, dtype, D, lens):
+    """Masked edges and edges of index -1 point at keys and values of NaN and infinity."""
+    p = problem(lens, 40, 2, 2, D, dtype, "edge")
+    p["indices"].clamp_(max=37)
+    want = dg.attend_edges(p["q"], p["k"], p["v"], p["offsets"], p["indices"], bias=p["bias"])
+    go = randn(5, *p["q"].shape, dtype=dtype)
+    args = (p["offsets"], p["indices"])
+    want_g = dg.attend_edges_grad(go, p["q"], p["k"], p["v"], want.out, want.lse, *args,
+                                  bias=p["bias"])
+    masked = p["bias"] == NINF
+    assert masked.any()
+    idx = torch.where(masked, 38, p["indices"])
+    idx[masked.nonzero()[::2].flatten()] = 39
+    for n in "kv":
+        p[n][38], p[n][39] = float("nan"), float("inf")
+    p["k"][39] = -float("inf")
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    got = dg.attend_edges(p["q"], p["k"], p["v"], p["offsets"], idx, bias=p["bias"], status=status)
+    assert torch.equal(got.out, want.out) and torch.equal(got.lse, want.lse)
+    got_g = dg.attend_edges_grad(go, p["q"], p["k"], p["v"], got.out, got.lse, p["offsets"], idx,
+                                 bias=p["bias"])
+    assert torch.equal(got_g.q, want_g.q) and torch.equal(got_g.bias, want_g.bias)
+    assert not got_g.k[38:].any() and not got_g.v[38:].any()
+    # (the keys' sums are cut elsewhere where other edges lie between theirs)
+    check_gradient(dg, dict(p, indices=idx), got)
+    # key row 0, which lanes without an edge read, holds NaN
+    p["indices"].clamp_(min=1)
+    want = dg.attend_edges(p["q"], p["k"], p["v"], *args, bias=p["bias"])
+    for n in "kv":
+        p[n][0] = float("nan")
+    idx = torch.where(masked, -1, p["indices"])
+    got = dg.attend_edges(p["q"], p["k"], p["v"], p["offsets"], idx, bias=p["bias"], status=status)
+    assert torch.equal(got.out, want.out) and torch.equal(got.lse, want.lse)
+    assert int(status) == 0
+
+
+def test_masks_of_the_types_lowest_value(dg):
+    """-FLT_MAX is a score like others: alone in a list its edges share the weight evenly,
+    beside ordinary scores they have none."""
+    low = torch.finfo(torch.float32).min
+    p = problem([4, 4, 300], 20, 2, 2, 8, torch.float32, "edge")
+    p["bias"] = torch.zeros(308, device=DEV)
+    p["bias"][:4] = low
+    p["bias"][4:6] = low
+    p["bias"][8:] = low
+    r = dg.attend_edges(p["q"], p["k"], p["v"], p["offsets"], p["indices"], bias=p["bias"])
+    idx = p["indices"].long()
+    for i, (a, b) in enumerate([(0, 4), (6, 8), (8, 308)]):
+        if i != 1:
+            want = p["v"][idx[a:b]].double().mean(0)
+            assert (r.out[i].double() - want).abs().max() <= 310 * U * 4
+            assert (r.lse[i] <= low * 0.99).all()
+    solo = dict(p, offsets=offsets_of([0, 2, 0]), indices=p["indices"][6:8].contiguous(), bias=None)
+    alone = dg.attend_edges(solo["q"], p["k"], p["v"], solo["offsets"], solo["indices"])
+    assert torch.allclose(r.out[1], alone.out[1], rtol=0, atol=8 * U * 8)
+
+
+def test_scores_that_overflow_give_nan_and_stay_in_their_row(dg):
+    p = problem([3, 5, 300], 20, 1, 1, 8, torch.float32)
+    want = dg.attend_edges(p["q"], p["k"], p["v"], p["offsets"], p["indices"])
+    p["q"][1] = float("inf")
+    got = dg.attend_edges(p["q"], p["k"], p["v"], p["offsets"], p["indices"])
+    assert got.out[1].isnan().all()
+    assert torch.equal(got.out[::2], want.out[::2]) and torch.equal(got.lse[::2], want.lse[::2])
+
+
+def test_large_scores(dg):
+    p = problem([7, 1, 500], 50, 2, 2, 32, torch.float32)
+    p["scale"] = 30.0
+    check_gradient(dg, p, check_forward(dg, p))
+
+
+def test_bad_indices_and_offsets_are_reported(dg):
+    p = problem([3, 5, 300, 2], 20, 2, 2, 8, torch.float32, "edge")
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    args = lambda: (p["q"], p["k"], p["v"], p["offsets"], p["indices"])  # noqa: E731
+    dg.attend_edges(*args(), bias=p["bias"], status=status)
+    assert int(status) == 0
+    p["indices"][1], p["indices"][100], p["indices"][9] = 20, -3, 2 ** 31 - 1
+    r = dg.attend_edges(*args(), bias=p["bias"], scale=p["scale"], status=status)
+    assert int(status) == 1
+    status.zero_()
+    dg.attend_edges_grad(r.out, *args()[:3], r.out, r.lse, *args()[3:], bias=p["bias"],
+                         status=status)
+    assert int(status) == 1
+    check_gradient(dg, p, check_forward(dg, p))  # such edges add nothing
+    good = p["offsets"].clone()
+    for at, value in ((1, -1), (2, 400), (3, 5), (4, 2 ** 40), (0, 9)):
+        p["offsets"] = good.clone()
+        p["offsets"][at] = value
+        status.zero_()
+        r = dg.attend_edges(*args(), bias=p["bias"], status=status)
+        assert int(status) & 2, (at, value)
+        dg.attend_edges_grad(r.out, *args()[:3], r.out, r.lse, *args()[3:], bias=p["bias"])
+        torch.cuda.synchronize()
+
+
+def test_nothing_at_all(dg):
+    z = torch.zeros(0, 2, 8, device=DEV)
+    off, idx = torch.zeros(1, dtype=torch.int64, device=DEV), \
+        torch.zeros(0, dtype=torch.int32, device=DEV)
+    r = dg.attend_edges(z, z, z, off, idx)
+    assert r.out.shape == (0, 2, 8)
+    q = randn(1, 3, 2, 8)
+    r = dg.attend_edges(q, z, z, offsets_of([0, 0, 0]), idx)
+    assert not r.out.any() and (r.lse == NINF).all()
+    k = randn(2, 4, 2, 8)
+    g = dg.attend_edges_grad(q, q, k, k, r.out, r.lse, offsets_of([0, 0, 0]), idx)
+    assert not g.q.any() and not g.k.any() and not g.v.any()
+
+
+def test_results_repeat_to_the_bit(dg):
+    p = problem([4] * 20000 + [9000], 700, 4, 2, 32, torch.bfloat16, "edge")
+    p["indices"] = (torch.rand(p["indices"].numel(), device=DEV, generator=rng(1)).pow(3)
+                    * 700).int()
+    run = lambda: dg.attend_edges(p["q"], p["k"], p["v"], p["offsets"], p["indices"],  # noqa: E731
+                                  bias=p["bias"])
+    a = run()
+    go = randn(3, *p["q"].shape, dtype=torch.bfloat16)
+    grad = lambda: dg.attend_edges_grad(go, p["q"], p["k"], p["v"], a.out, a.lse,  # noqa: E731
+                                        p["offsets"], p["indices"], bias=p["bias"])
+    ga = grad()
+    for _ in range(3):
+        b, gb = run(), grad()
+        assert torch.equal(a.out, b.out) and torch.equal(a.lse, b.lse)
+        for n in ("q", "k", "v", "bias"):
+            assert torch.equal(getattr(ga, n), getattr(gb, n)), n
+
+
+def test_gradient_against_differences(dg):
+    """Along random directions of q, k, v and the bias, in 32 bits with a step for which the
+    third-order term and the rounding are both below 2e-3 of the change."""
+    p = problem([4, 0, 9, 1, 200], 25, 4, 2, 12, torch.float32, "edge")
+    go = randn(9, *p["q"].shape)
+    fwd = dg.attend_edges(p["q"], p["k"], p["v"], p["offsets"], p["indices"], bias=p["bias"])
+    g = dg.attend_edges_grad(go, p["q"], p["k"], p["v"], fwd.out, fwd.lse, p["offsets"],
+                             p["indices"], bias=p["bias"])
+
+    def loss(**change):
+        x = dict(p, **change)
+        r = dg.attend_edges(x["q"], x["k"], x["v"], x["offsets"], x["indices"], bias=x["bias"])
+        return float((r.out.double() * go.double()).sum())
+
+    eps = 1e-2
+    for n in ("q", "k", "v", "bias"):
+        for seed in range(3):
+            d = randn(30 + seed, *p[n].shape)
+            moved = (loss(**{n: p[n] + eps * d}) - loss(**{n: p[n] - eps * d})) / (2 * eps)
+            grad = getattr(g, n).double()
+            want = float((grad * d.double()).sum())
+            assert abs(moved - want) <= 2e-3 * float(grad.norm() * d.double().norm()), n
+
+
+@pytest.mark.big
+def test_rows_past_32_bit_offsets(dg):
+    """Key rows whose offsets pass 2^32 elements, by a stride into one large buffer."""
+    nkv, heads, D, stride = 1 << 20, 2, 32, 4104
+    buf = torch.zeros(nkv * stride, dtype=torch.bfloat16, device=DEV)
+    rows = buf.view(nkv, stride)
+    k = rows[:, :heads * D].unflatten(1, (heads, D))
+    v = rows[:, 100:100 + heads * D].unflatten(1, (heads, D))
+    lens = [5, 7, 300]
+    idx = nkv - 1 - torch.randperm(400, device=DEV)[:sum(lens)].int() * 3
+    k[-1200:], v[-1200:] = randn(1, 1200, heads, D).bfloat16(), randn(2, 1200, heads, D).bfloat16()
+    q = randn(3, 3, heads, D).bfloat16()
+    a = dg.attend_edges(q, k, v, offsets_of(lens), idx.int())
+    b = dg.attend_edges(q, k[-1200:].contiguous(), v[-1200:].contiguous(), offsets_of(lens),
+                        (idx - (nkv - 1200)).int())
+    assert torch.equal(a.out, b.out) and torch.equal(a.lse, b.lse)
+
+
+# ------------------------------------------------------------------------ edge lists
+@pytest.mark.parametrize("E", [0, 1, 255, 256, 5000, 100_001])
+@pytest.mark.parametrize("rows", [0, 1, 255, 256, 257, 3000])
+def test_edge_offsets(dg, E, rows):
+    if rows == 0 and E:
+        return
+    src = torch.randint(0, max(rows, 1), (E,), device=DEV, generator=rng(E + rows)).sort().values
+    if E > 10 and rows > 10:
+        src = torch.where(src % 3 == 0, src // 2, src).sort().values  # gaps
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    got = dg.edge_offsets(src.int(), rows, status=status)
+    want = torch.searchsorted(src, torch.arange(rows + 1, device=DEV))
+    assert torch.equal(got, want) and int(status) == 0
+
+
+def test_edge_offsets_reports_bad_edges(dg):
+    for src in ([0, 2, 1], [0, 1, 5], [-1, 0, 1]):
+        status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        off = dg.edge_offsets(torch.tensor(src, dtype=torch.int32, device=DEV), 5, status=status)
+        assert int(status) == 2 and off.min() >= 0 and off.max() <= 3
+
+
+def test_refusals(dg):
+    p = problem([3, 5], 20, 4, 2, 8, torch.float32, "edge")
+    q, k, v, off, idx = p["q"], p["k"], p["v"], p["offsets"], p["indices"]
+    for bad in ((q.double(), k, v, off, idx), (q, k.half(), v, off, idx),
+                (q, k, v, off.int(), idx), (q, k, v, off, idx.long())):
+        with pytest.raises(TypeError):
+            dg.attend_edges(*bad)
+    for bad in ((q[0], k, v, off, idx), (q, k[:, :, :4], v, off, idx), (q, k, v[:5], off, idx),
+                (q, k, v, off[:2], idx), (q.transpose(1, 2), k, v, off, idx),
+                (q, k.cpu(), v, off, idx)):
+        with pytest.raises(ValueError):
+            dg.attend_edges(*bad)
+    with pytest.raises(ValueError):
+        dg.attend_edges(q, k, v, off, idx, bias=p["bias"][:3])
+    with pytest.raises(dg.DGError):
+        dg.attend_edges(q, k[:, [0, 1, 1]].contiguous(), v[:, [0, 1, 1]].contiguous(), off, idx)
+    big = torch.zeros(2, 1, 300, device=DEV)
+    with pytest.raises(dg.DGError):
+        dg.attend_edges(big, big, big, off, idx)
+    r = dg.attend_edges(q, k, v, off, idx)
+    with pytest.raises(ValueError):
+        dg.attend_edges_grad(q[:1], q, k, v, r.out, r.lse, off, idx)
+    with pytest.raises(ValueError):
+        dg.attend_edges_grad(q, q, k, v, r.out, r.lse[:1], off, idx)
+
+
+# ------------------------------------------------------------------------ streams and graphs
+def test_on_another_stream(dg):
+    """Work and its temporaries on a given stream, behind that stream's own earlier work."""
+    p = problem([5] * 4000 + [3000], 900, 4, 2, 32, torch.float32, "edge")
+    args = (p["offsets"], p["indices"])
+    want = dg.attend_edges(p["q"], p["k"], p["v"], *args, bias=p["bias"])
+    want_g = dg.attend_edges_grad(p["q"], p["q"], p["k"], p["v"], want.out, want.lse, *args,
+                                  bias=p["bias"])
+    ids = p["indices"]
+    want_e = dg.embed_rows_grad(randn(4, ids.numel(), 16), ids, 900)
+    late = torch.zeros_like(p["q"])
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+        late.copy_(p["q"])
+    got = dg.attend_edges(late, p["k"], p["v"], *args, bias=p["bias"], stream=s)
+    got_g = dg.attend_edges_grad(late, late, p["k"], p["v"], got.out, got.lse, *args,
+                                 bias=p["bias"], stream=s)
+    with torch.cuda.stream(s):
+        got_e = dg.embed_rows_grad(randn(4, ids.numel(), 16), ids, 900)
+    s.synchronize()
+    assert torch.equal(got.out, want.out) and torch.equal(got_e, want_e)
+    for n in ("q", "k", "v", "bias"):
+        assert torch.equal(getattr(got_g, n), getattr(want_g, n)), n
+
+
+def test_in_a_graph(dg):
+    """A step of all operators captured once and replayed on new inputs."""
+    N, D, heads = 500, 64, 4
+    p = problem([6] * 700 + [300], 700, heads, heads, D // heads, torch.float32, "edge")
+    nq = p["q"].shape[0]
+    table, w = randn(1, N, D), randn(2, D)
+    ids = torch.randint(0, N, (nq,), device=DEV, dtype=torch.int32, generator=rng(3))
+    p["indices"] = torch.randint(0, nq, p["indices"].shape, device=DEV, dtype=torch.int32,
+                                 generator=rng(4))
+
+    def step():
+        x = dg.embed_rows(table, ids, scale=2.0)
+        r = dg.norm_rows(x, w)
+        h = r.y.view(nq, heads, -1)
+        a = dg.attend_edges(h, h, h, p["offsets"], p["indices"], bias=p["bias"])
+        g = dg.attend_edges_grad(a.out, h, h, h, a.out, a.lse, p["offsets"], p["indices"],
+                                 bias=p["bias"])
+        gx, gw = dg.norm_rows_grad((g.q + g.k + g.v).view(nq, D), r.h, r.rstd, w)
+        return a.out, gx, gw, dg.embed_rows_grad(gx, ids, N, scale=2.0)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for seed in range(4):
+        table.copy_(randn(10 + seed, N, D))
+        ids.copy_(torch.randint(0, N, (nq,), device=DEV, dtype=torch.int32, generator=rng(seed)))
+        want = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(outs, want):
+            assert torch.equal(x, y)

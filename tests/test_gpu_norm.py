@@ -1,0 +1,256 @@
+"""RMS norm of rows and its gradient against the formulas in 64 bits.
+
+Tolerances.  A sum of D products in 32 bits is off by at most (D + 1) 2^-24 of the sum of
+magnitudes; the kernels add in trees, but the bound of any order is used.  So rstd is off by
+(D + 8) 2^-24 of its value, y by (D + 12) 2^-24, both before y's rounding to its type
+(half a unit: 2^-24, 2^-11, 2^-8 of the value).  An 8-bit code is within half a step of
+y / c: 2^-4 of its value, or 2^-10 below 2^-6 (e4m3 has 3 mantissa bits, smallest step
+2^-9), and c = max|y| / 448 as exact as y."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+F8 = torch.float8_e4m3fn
+HALF_UNIT = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+WIDE = list(HALF_UNIT)
+TINY = 2.0 ** -25  # half the smallest 16-bit step
+
+
+@pytest.fixture(scope="module")
+def dg():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2405_05231_amd as m
+    return m
+
+
+def randn(seed, *shape, dtype=torch.float32):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return torch.randn(*shape, device=DEV, generator=g).to(dtype)
+
+
+def plain(x, w, res, eps):
+    h = x.double() if res is None else x.double() + res.double()
+    rstd = (h.square().mean(1) + eps).rsqrt()
+    return h, rstd, h * rstd[:, None] * w.double()
+
+
+def close(got, want, tol):
+    bad = (got.double() - want).abs() > tol
+    assert not bad.any(), (got[bad][:4], want[bad][:4])
+
+
+def check_forward(dg, x, w, res, to, group, eps=1e-6):
+    n, D = x.shape
+    r = dg.norm_rows(x, w, residual=res, eps=eps, dtype=to, group=group)
+    h, rstd, y = plain(x, w, res, eps)
+    unit = HALF_UNIT[x.dtype]
+    rel = (D + 12) * 2.0 ** -24
+    if res is None:
+        assert r.h is x
+    else:
+        # the sum is rounded to 32 bits, then to the type
+        close(r.h, h, (unit + 2.0 ** -23) * h.abs() + TINY)
+    close(r.rstd, rstd, rel * rstd)
+    if to != F8:
+        assert r.scale is None and r.y.dtype == x.dtype
+        close(r.y, y, (unit + 2 * rel) * y.abs() + TINY)
+        return
+    size = group if group else D
+    parts = -(-D // size)
+    assert r.y.dtype == F8 and tuple(r.scale.shape) == (n, parts)
+    pad = torch.nn.functional.pad(y, (0, parts * size - D)).view(n, parts, size)
+    c = pad.abs().amax(2) / 448
+    close(r.scale, c, 2 * rel * c)
+    c = c.repeat_interleave(size, 1)[:, :D]
+    code = r.y.float().double()
+    q = torch.where(c > 0, y / torch.where(c > 0, c, 1.0), 0.0)
+    close(code, q, (2.0 ** -4 + 4 * rel) * q.abs() + 2.0 ** -10)
+
+
+DIMS = [1, 3, 4, 7, 8, 9, 16, 31, 64, 100, 128, 200, 256, 385, 512, 602, 768, 1024, 1025, 2048,
+        2049, 5000, 9001]
+
+
+@pytest.mark.parametrize("D", DIMS)
+@pytest.mark.parametrize("dtype", WIDE)
+@pytest.mark.parametrize("with_res", [False, True])
+def test_norm(dg, D, dtype, with_res):
+    n = 37
+    x = randn(1, n, D, dtype=dtype)
+    res = randn(2, n, D, dtype=dtype) if with_res else None
+    w = randn(3, D)
+    check_forward(dg, x, w, res, dtype, 0)
+    for group in (0, 32, 64, 128):
+        check_forward(dg, x, w, res, F8, group)
+
+
+@pytest.mark.parametrize("n", [0, 1, 2, 3, 255, 256, 257, 5000])
+@pytest.mark.parametrize("D", [16, 128, 768])
+def test_norm_lengths(dg, n, D):
+    x, w, res = randn(1, n, D, dtype=torch.bfloat16), randn(3, D), \
+        randn(2, n, D, dtype=torch.bfloat16)
+    check_forward(dg, x, w, res, torch.bfloat16, 0)
+    check_forward(dg, x, w, res, F8, 128)
+
+
+@pytest.mark.parametrize("dtype", WIDE)
+def test_norm_of_strided_rows(dg, dtype):
+    x, res = randn(1, 50, 150, dtype=dtype)[:, 5:106], randn(2, 50, 120, dtype=dtype)[:, 3:104]
+    check_forward(dg, x, randn(3, 101), res, dtype, 0)
+    check_forward(dg, x, randn(3, 101), res, F8, 32)
+
+
+@pytest.mark.parametrize("D", [8, 100, 768, 5000])
+def test_norm_of_zero_tiny_and_huge_rows(dg, D):
+    x = randn(1, 6, D)
+    x[0] = 0
+    x[1] *= 1e-30  # far below eps: y is tiny
+    x[2] *= 1e-18
+    x[3] *= 1e15
+    x[4] = 0
+    x[4, D // 2] = 1e-35
+    w = randn(2, D)
+    for group in (0, 32):
+        check_forward(dg, x, w, None, F8, group)
+    check_forward(dg, x, w, None, torch.float32, 0)
+    # scales below 2^-100, values above the smallest normal number
+    check_forward(dg, x[[2, 3, 5]], w * 1e-18, None, F8, 0)
+    r = dg.norm_rows(x, w, dtype=F8)
+    assert not r.y[0].float().any() and float(r.scale[0]) == 0
+    # eps = 0: a zero row is 0 * infinity
+    r = dg.norm_rows(x, w, eps=0.0)
+    assert r.y[0].isnan().all() and r.y[3].isfinite().all()
+
+
+@pytest.mark.parametrize("D", [64, 385, 5000])
+def test_norm_keeps_nan_and_infinity_in_their_rows(dg, D):
+    x = randn(1, 4, D)
+    x[1, 3] = float("nan")
+    x[2, D - 1] = float("inf")
+    w = randn(2, D)
+    r = dg.norm_rows(x, w)
+    assert r.y[1].isnan().all() and r.rstd[1].isnan()
+    assert r.y[2, D - 1].isnan() and not r.y[2, :D - 1].any() and r.rstd[2] == 0
+    for group in (0, 64):
+        q = dg.norm_rows(x, w, dtype=F8, group=group)
+        assert q.y[1].float().isnan().all() and q.scale[1].isnan().all()
+        assert q.y[2, D - 1].float().isnan() and q.scale[2, -1].isnan()
+        check_forward(dg, x[::3].contiguous(), w, None, F8, group)
+    # a group beside the infinity holds zeros
+    assert not q.y[2, :64 * ((D - 1) // 64)].float().any()
+
+
+def test_8_bit_rows_can_be_looked_up_again(dg):
+    """A norm's 8-bit rows and their scales are a table of dg.embed_rows."""
+    x, w = randn(1, 300, 256), randn(2, 256)
+    r = dg.norm_rows(x, w, dtype=F8)
+    ids = torch.randperm(300, device=DEV).int()
+    got = dg.embed_rows(r.y, ids, row_scale=r.scale.view(-1))
+    assert torch.equal(got, (r.y.float() * r.scale)[ids.long()])
+
+
+# ------------------------------------------------------------------------ gradient
+def plain_grad(gy, h, rstd, w, gh):
+    gy, h, w, r = gy.double(), h.double(), w.double(), rstd.double()[:, None]
+    u, g = h * r, gy * w
+    gx = r * (g - u * (g * u).mean(1, keepdim=True))
+    mag = r * (g.abs() + u.abs() * (g * u).abs().mean(1, keepdim=True))
+    if gh is not None:
+        gx, mag = gx + gh.double(), mag + gh.double().abs()
+    return gx, mag, (gy * u).sum(0), (gy * u).abs().sum(0)
+
+
+def check_grad(dg, gy, h, w, gh):
+    n, D = gy.shape
+    rstd = (h.float().square().mean(1) + 1e-6).rsqrt()
+    gx, gw = dg.norm_rows_grad(gy, h, rstd, w, grad_h=gh)
+    x64, xm, w64, wm = plain_grad(gy, h, rstd, w, gh)
+    rel = (D + 12) * 2.0 ** -24
+    close(gx, x64, HALF_UNIT[gy.dtype] * (1 + rel) * x64.abs() + 2 * rel * xm + TINY)
+    close(gw, w64, (n + 4) * 2.0 ** -24 * wm + 1e-30)
+
+
+@pytest.mark.parametrize("D", DIMS)
+@pytest.mark.parametrize("dtype", WIDE)
+@pytest.mark.parametrize("with_gh", [False, True])
+def test_norm_gradient(dg, D, dtype, with_gh):
+    n = 53
+    check_grad(dg, randn(1, n, D, dtype=dtype), randn(2, n, D, dtype=dtype), randn(3, D),
+               randn(4, n, D, dtype=dtype) if with_gh else None)
+
+
+@pytest.mark.parametrize("n", [0, 1, 2, 7, 1024, 4095, 20001])
+@pytest.mark.parametrize("D", [5, 128, 385, 5000])
+def test_norm_gradient_lengths(dg, n, D):
+    if n * D > 30_000_000:
+        n = 3001  # more rows than blocks all the same
+    check_grad(dg, randn(1, n, D), randn(2, n, D), randn(3, D), None)
+
+
+def test_norm_gradient_of_strided_rows(dg):
+    big = randn(1, 3, 400, 150, dtype=torch.bfloat16)
+    check_grad(dg, big[0][:, 1:102], big[1][:, 9:110], randn(3, 101), big[2][:, 40:141])
+
+
+def test_norm_gradient_repeats_to_the_bit(dg):
+    gy, h, w = randn(1, 30000, 128), randn(2, 30000, 128), randn(3, 128)
+    rstd = torch.rand(30000, device=DEV)
+    a = dg.norm_rows_grad(gy, h, rstd, w)
+    for _ in range(3):
+        b = dg.norm_rows_grad(gy, h, rstd, w)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_norm_gradient_against_differences(dg):
+    """Along random directions of x, the residual and the weight, in 32 bits with a step for
+    which the third-order term and the rounding are both below 1e-3 of the change."""
+    n, D = 40, 96
+    x, res, w = randn(1, n, D), randn(2, n, D), 1 + 0.1 * randn(3, D)
+    gy = randn(4, n, D)
+    fwd = dg.norm_rows(x, w, residual=res)
+    gx, gw = dg.norm_rows_grad(gy, fwd.h, fwd.rstd, w)
+
+    def loss(x, res, w):
+        return float((dg.norm_rows(x, w, residual=res).y.double() * gy.double()).sum())
+
+    eps = 1e-2
+    for seed in range(4):
+        dx, dw = randn(10 + seed, n, D), randn(20 + seed, D)
+        for up, down, along in (
+                (loss(x + eps * dx, res, w), loss(x - eps * dx, res, w), (gx, dx)),
+                (loss(x, res + eps * dx, w), loss(x, res - eps * dx, w), (gx, dx)),
+                (loss(x, res, w + eps * dw), loss(x, res, w - eps * dw), (gw, dw))):
+            want = float((along[0].double() * along[1].double()).sum())
+            scale = float(along[0].double().norm() * along[1].double().norm())
+            assert abs((up - down) / (2 * eps) - want) <= 1e-3 * scale
+
+
+def test_refusals(dg):
+    x, w = randn(1, 4, 8), randn(2, 8)
+    with pytest.raises(TypeError):
+        dg.norm_rows(x.double(), w)
+    with pytest.raises(TypeError):
+        dg.norm_rows(x, w.half())
+    with pytest.raises(TypeError):
+        dg.norm_rows(x, w, residual=x.half())
+    with pytest.raises(TypeError):
+        dg.norm_rows(x, w, dtype=torch.int8)
+    with pytest.raises(ValueError):
+        dg.norm_rows(x, randn(2, 9))
+    with pytest.raises(ValueError):
+        dg.norm_rows(x, w, residual=randn(1, 5, 8))
+    with pytest.raises(ValueError):
+        dg.norm_rows(x.t(), randn(2, 4))
+    with pytest.raises(dg.DGError):
+        dg.norm_rows(x, w, dtype=torch.float16)
+    with pytest.raises(dg.DGError):
+        dg.norm_rows(x, w, dtype=F8, group=48)
+    with pytest.raises(dg.DGError):
+        dg.norm_rows(x, w, eps=-1.0)
+    with pytest.raises(ValueError):
+        dg.norm_rows_grad(x, x, randn(1, 3), w)
+    with pytest.raises(TypeError):
+        dg.norm_rows_grad(x, x.half(), randn(1, 4), w)

@@ -1,0 +1,207 @@
+"""Argument checks and workspace queries of the model-row operators on the host side (no
+GPU): every refusal happens before any device work, so the pointers may be anything."""
+import ctypes
+
+import pytest
+
+F32, F16, BF16, F8 = 0, 1, 2, 3
+P = 0x10000  # a pointer that is never followed
+GAP = 1 << 34
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2405_05231_amd import _lib
+    return _lib.load()
+
+
+def at(i):
+    """Far-apart 256-aligned addresses."""
+    return P + i * GAP
+
+
+def expect(L, status, want, word=None):
+    assert status == want, L.dg_last_error()
+    if word:
+        assert word in L.dg_last_error().decode()
+
+
+def call(fn, args, **change):
+    """fn(**args) with some arguments replaced; args keep the order of the C ABI."""
+    assert set(change) <= set(args)
+    return fn(*{**args, **change}.values())
+
+
+EMBED = dict(table=at(1), table_type=F32, N=10, D=8, stride=8, row_scale=None, ids=at(2), n=4,
+             scale=1.0, out=at(3), out_type=F32, out_stride=8, status=None, stream=None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(N=0), dict(N=1 << 31), dict(D=0), dict(D=65537), dict(n=-1), dict(stride=7),
+    dict(out_stride=7), dict(table_type=4), dict(table_type=-1), dict(out_type=F8),
+    dict(table=None), dict(ids=None), dict(out=None), dict(out=at(1)), dict(out=at(1) + 4 * 79),
+    dict(out=at(2)), dict(row_scale=at(3) + 8)])
+def test_embed_rows_refuses(L, change):
+    expect(L, call(L.dg_embed_rows, EMBED, **change), -1)
+
+
+def test_embed_rows_of_nothing(L):
+    expect(L, call(L.dg_embed_rows, EMBED, n=0, table=None, ids=None, out=None), 0)
+
+
+EGRAD = dict(grad_out=at(1), type=F32, stride=8, ids=at(2), n=4, N=10, D=8, scale=1.0, grad=at(3),
+             grad_type=F32, rows=None, num_rows=None, status=None, ws=at(4), ws_bytes=1 << 30,
+             stream=None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(N=0), dict(N=1 << 31), dict(D=0), dict(D=65537), dict(n=-1), dict(n=1 << 31),
+    dict(stride=7), dict(type=F8), dict(grad_type=F8), dict(type=7), dict(grad_out=None),
+    dict(ids=None), dict(grad=None), dict(rows=at(5)), dict(num_rows=at(5)), dict(grad=at(1)),
+    dict(grad=at(2)), dict(rows=at(2), num_rows=at(5))])
+def test_embed_rows_grad_refuses(L, change):
+    expect(L, call(L.dg_embed_rows_grad, EGRAD, **change), -1)
+
+
+@pytest.mark.parametrize("change", [dict(ws=None), dict(ws_bytes=0), dict(ws=at(4) + 8)])
+@pytest.mark.parametrize("sparse", [False, True])
+def test_embed_rows_grad_refuses_its_workspace(L, change, sparse):
+    more = dict(rows=at(5), num_rows=at(6)) if sparse else {}
+    expect(L, call(L.dg_embed_rows_grad, EGRAD, **change, **more), -4, "workspace needs")
+
+
+NORM = dict(x=at(1), x_stride=8, residual=at(2), res_stride=8, type=F32, n=4, D=8, weight=at(3),
+            eps=1e-6, y=at(4), y_type=F32, group=0, scales=None, h=at(5), rstd=at(6), stream=None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(n=-1), dict(n=1 << 31), dict(D=0), dict(D=65537), dict(x_stride=7), dict(res_stride=7),
+    dict(type=F8), dict(type=9), dict(y_type=F16), dict(y_type=9), dict(group=16), dict(group=-1),
+    dict(eps=-1.0), dict(eps=float("nan")), dict(x=None), dict(weight=None), dict(y=None),
+    dict(y_type=F8), dict(y=at(1)), dict(y=at(2)), dict(y=at(3)), dict(y=at(5)), dict(h=at(1) + 4),
+    dict(h=at(1), x_stride=9), dict(h=at(2) + 4)])
+def test_norm_rows_refuses(L, change):
+    expect(L, call(L.dg_norm_rows, NORM, **change), -1)
+
+
+def test_norm_rows_of_nothing(L):
+    expect(L, call(L.dg_norm_rows, NORM, n=0), 0)
+
+
+NGRAD = dict(grad_y=at(1), stride=8, h=at(2), h_stride=8, rstd=at(3), weight=at(4), grad_h=at(5),
+             gh_stride=8, type=F32, n=4, D=8, grad_x=at(6), grad_weight=at(7), ws=at(8),
+             ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(n=-1), dict(n=1 << 31), dict(D=0), dict(D=65537), dict(stride=7), dict(h_stride=7),
+    dict(gh_stride=7), dict(type=F8), dict(grad_y=None), dict(h=None), dict(rstd=None),
+    dict(weight=None), dict(grad_x=None), dict(grad_weight=None), dict(grad_x=at(2)),
+    dict(grad_x=at(1), stride=9), dict(grad_x=at(5) + 4), dict(grad_weight=at(4))])
+def test_norm_rows_grad_refuses(L, change):
+    expect(L, call(L.dg_norm_rows_grad, NGRAD, **change), -1)
+
+
+@pytest.mark.parametrize("change", [dict(ws=None), dict(ws_bytes=0), dict(ws=at(8) + 8)])
+def test_norm_rows_grad_refuses_its_workspace(L, change):
+    expect(L, call(L.dg_norm_rows_grad, NGRAD, **change), -4, "workspace needs")
+
+
+OFFSETS = dict(edge_src=at(1), num_edges=8, num_rows=4, offsets=at(2), status=None, stream=None)
+
+
+@pytest.mark.parametrize("change", [dict(num_edges=-1), dict(num_edges=1 << 31), dict(num_rows=-1),
+                                    dict(num_rows=1 << 31), dict(edge_src=None),
+                                    dict(offsets=None), dict(offsets=at(1))])
+def test_edge_offsets_refuses(L, change):
+    expect(L, call(L.dg_edge_offsets, OFFSETS, **change), -1)
+
+
+ATTEND = dict(q=at(1), q_stride=16, k=at(2), k_stride=8, v=at(3), v_stride=8, type=F32, nq=4, nkv=5,
+              heads=4, kv_heads=2, D=4, offsets=at(4), indices=at(5), num_edges=1000, bias=at(6),
+              bias_heads=1, scale=0.5, out=at(7), lse=at(8), status=None, ws=at(9),
+              ws_bytes=1 << 30, stream=None)
+SIZES = [dict(nq=-1), dict(nq=1 << 31), dict(nkv=-1), dict(nkv=1 << 31), dict(num_edges=-1),
+         dict(num_edges=1 << 31), dict(nkv=0), dict(heads=0), dict(kv_heads=0), dict(heads=3),
+         dict(heads=2048, kv_heads=1024), dict(D=0), dict(D=257), dict(type=F8), dict(type=5),
+         dict(bias_heads=2), dict(q_stride=15), dict(k_stride=7), dict(v_stride=7), dict(q=None),
+         dict(k=None), dict(v=None), dict(indices=None), dict(offsets=None)]
+
+
+@pytest.mark.parametrize("change", SIZES + [
+    dict(out=None), dict(lse=None), dict(out=at(1)), dict(out=at(2)), dict(out=at(3)),
+    dict(out=at(4)), dict(out=at(5)), dict(out=at(8)), dict(lse=at(6))])
+def test_attend_edges_refuses(L, change):
+    expect(L, call(L.dg_attend_edges, ATTEND, **change), -1)
+
+
+@pytest.mark.parametrize("change", [dict(ws=None), dict(ws_bytes=0), dict(ws=at(9) + 8)])
+def test_attend_edges_refuses_its_workspace(L, change):
+    expect(L, call(L.dg_attend_edges, ATTEND, **change), -4, "workspace needs")
+
+
+def test_attend_edges_of_nothing(L):
+    expect(L, call(L.dg_attend_edges, ATTEND, nq=0, num_edges=0, q=None, offsets=None, out=None,
+                   lse=None), 0)
+
+
+AGRAD = dict(grad_out=at(1), g_stride=16, q=at(2), q_stride=16, k=at(3), k_stride=8, v=at(4),
+             v_stride=8, out=at(5), out_stride=16, lse=at(6), type=F32, nq=4, nkv=5, heads=4,
+             kv_heads=2, D=4, offsets=at(7), indices=at(8), num_edges=1000, bias=at(9),
+             bias_heads=1, scale=0.5, grad_q=at(10), grad_k=at(11), grad_v=at(12),
+             grad_bias=at(13), status=None, ws=at(14), ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("change", SIZES + [
+    dict(g_stride=15), dict(out_stride=15), dict(grad_out=None), dict(out=None), dict(lse=None),
+    dict(grad_q=None), dict(grad_k=None), dict(grad_v=None), dict(bias=None), dict(grad_q=at(2)),
+    dict(grad_k=at(3)), dict(grad_v=at(4)), dict(grad_bias=at(9)), dict(grad_q=at(8)),
+    dict(grad_v=at(11)), dict(grad_bias=at(10))])
+def test_attend_edges_grad_refuses(L, change):
+    expect(L, call(L.dg_attend_edges_grad, AGRAD, **change), -1)
+
+
+@pytest.mark.parametrize("change", [dict(ws=None), dict(ws_bytes=0), dict(ws=at(14) + 8)])
+def test_attend_edges_grad_refuses_its_workspace(L, change):
+    expect(L, call(L.dg_attend_edges_grad, AGRAD, **change), -4, "workspace needs")
+
+
+def lengths():
+    steps = [1, 128, 2048, 1 << 17, 1 << 18, 1 << 19, 1 << 20, 1 << 21]
+    return sorted({0, 3 << 22, *(s + d for s in steps for d in (-1, 0, 1))})
+
+
+def test_workspaces_never_shrink_with_the_list(L):
+    for sparse in (0, 1):
+        got = [L.dg_embed_rows_grad_workspace_bytes(1000, 128, n, sparse) for n in lengths()]
+        assert got == sorted(got) and got[0] > 0
+    got = [L.dg_norm_rows_grad_workspace_bytes(n, 128) for n in lengths()]
+    assert got == sorted(got) and got[0] > 0
+    got = [L.dg_attend_edges_workspace_bytes(n, 4, 32) for n in lengths()]
+    assert got == sorted(got) and got[0] > 0
+    got = [L.dg_attend_edges_grad_workspace_bytes(n, 1000, 4, 2, 32) for n in lengths()]
+    assert got == sorted(got) and got[0] > 0
+
+
+def test_workspace_queries_refuse(L):
+    assert L.dg_embed_rows_grad_workspace_bytes(0, 128, 10, 0) == 0
+    assert L.dg_embed_rows_grad_workspace_bytes(10, 0, 10, 0) == 0
+    assert L.dg_embed_rows_grad_workspace_bytes(10, 8, -1, 1) == 0
+    assert L.dg_norm_rows_grad_workspace_bytes(-1, 8) == 0
+    assert L.dg_norm_rows_grad_workspace_bytes(1, 1 << 20) == 0
+    assert L.dg_attend_edges_workspace_bytes(-1, 1, 8) == 0
+    assert L.dg_attend_edges_workspace_bytes(1, 0, 8) == 0
+    assert L.dg_attend_edges_grad_workspace_bytes(1, 1, 1, 2, 8) == 0
+    assert L.dg_attend_edges_grad_workspace_bytes(1, 1, 2, 1, 300) == 0
+
+
+def test_types_have_the_headers_numbers():
+    import os
+    import re
+
+    from conftest import ROOT
+    from paper_2405_05231_amd import _lib
+    text = open(os.path.join(ROOT, "include", "dg.h")).read()
+    for name in ("DG_F32", "DG_F16", "DG_BF16", "DG_F8E4M3"):
+        assert int(re.search(rf"\b{name} = (\d+)", text).group(1)) == getattr(_lib, name)
+    assert ctypes.sizeof(ctypes.c_float) == 4
