@@ -592,6 +592,7 @@ typedef enum dg_dtype {
 #define DG_MAX_COLS 65536    /* columns of a row of dg_embed_rows, dg_norm_rows */
 #define DG_MAX_HEADS 1024    /* query heads of dg_attend_edges */
 #define DG_MAX_HEAD_DIM 256  /* elements of a head */
+#define DG_MAX_STRIDE 536870912 /* between rows of keys or values of dg_attend_edges */
 
 /* Embedding rows: out[i] = scale * row_scale[ids[i]] * table[ids[i]], i in [0, n).
  *   table      [N] rows of D elements of table_type (any dg_dtype).

@@ -21,6 +21,8 @@
 // length, a wave per chunk, and joined by a second launch.
 #include <string.h>
 
+#include <algorithm>
+
 #include "dg_segments.h"
 
 namespace dg {
@@ -33,7 +35,8 @@ constexpr float NINF = -__builtin_inff();
 
 struct Attend {
   const void *q, *k, *v;
-  int64_t q_stride, k_stride, v_stride;
+  int64_t q_stride;
+  uint32_t k_bytes, v_bytes;  // between rows
   const int64_t *offsets;
   const int32_t *indices;
   const float *bias;   // [edges][bias_heads] or NULL
@@ -42,11 +45,13 @@ struct Attend {
   int heads, kv_heads, share, D;
   float scale;
   int lg_g, lg_h, lg_e;
-  int64_t row_blocks;  // blocks that take rows; the others take chunks
-  int64_t chunks;      // 0: no list can be longer than ch
+  int rounds;            // rows that a lane's row slot takes one after the other
+  int64_t chunk_blocks;  // the first blocks take chunks, the others rows
+  int64_t chunks;        // 0: no list can be longer than ch
   int ch;
-  int64_t slot;        // numbers of a partial result
-  float *part;         // [2 * chunks][slot]
+  int64_t slot;          // numbers of a partial result
+  float *part;           // [2 * chunks][slot]
+  int64_t *starts;       // [chunks] the long list's row that starts in the chunk, -1: none
   int32_t *status;
   // forward
   void *out;
@@ -55,12 +60,28 @@ struct Attend {
   const void *go, *o;
   int64_t go_stride, o_stride;
   const float *lse_in;
-  float2 *pd;          // [edges][heads] p and ds
-  int32_t *row_of;     // [edges]
+  const int32_t *place;  // [edges] place of each edge in the order of the keys
+  float2 *pd;            // [edges][heads] p and ds, in that order
+  int32_t *row_of;       // [edges] row, in that order
   void *dq;
+  float *db;             // [edges][bias_heads] or NULL
 };
 
+constexpr int CAP = 256;  // edges whose numbers a wave keeps in shared memory
+
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
+
+// Sum of products of two vectors as they lie in memory.
+template <typename T, int V>
+__device__ __forceinline__ float dot(const Raw<T, V> &x, const Raw<T, V> &y) {
+  float a[V], b[V];
+  to_floats<T, V>(x, a);
+  to_floats<T, V>(y, b);
+  float d = a[0] * b[0];
+#pragma unroll
+  for (int i = 1; i < V; ++i) d += a[i] * b[i];
+  return d;
+}
 
 // What a lane is for.
 template <typename T, int V, int RT>
@@ -69,7 +90,10 @@ struct Lane {
   int es, rs;       // edge and row within the wave
   int kvh, h0;      // key head, first query head
   bool head;        // whether there is such a head
+  bool first;       // first lane of its head
   bool ragged;      // elements of a key may be foreign
+  const char *k, *v;  // its vector of row 0 of the keys and values
+  typename Raw<T, V>::W mask;  // ones where the element is this lane's own
   __device__ __forceinline__ Lane(const Attend &a, int lg_e)
       : pc((int)(threadIdx.x & ((1 << a.lg_g) - 1)), a.D) {
     const int lane = threadIdx.x & 63;
@@ -81,29 +105,35 @@ struct Lane {
     head = h < a.kv_heads;
     kvh = min(h, a.kv_heads - 1);
     h0 = kvh * a.share + (blockIdx.y - tile * parts) * RT;
+    first = (lane & ((1 << a.lg_g) - 1)) == 0;
     ragged = (V << a.lg_g) != a.D;
+    k = (const char *)(static_cast<const T *>(a.k) + kvh * a.D + pc.at);
+    v = (const char *)(static_cast<const T *>(a.v) + kvh * a.D + pc.at);
+    typedef std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t> Word;
+    Word m[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) m[i] = pc.own(i) && pc.at + i < a.D ? (Word)~0u : (Word)0;
+    memcpy(&mask, m, sizeof(m));
+  }
+  // A vector with foreign elements 0 (they meet zeros in a product, but may be infinite).
+  __device__ __forceinline__ Raw<T, V> own(Raw<T, V> x) const {
+    if (ragged) x.w &= mask;
+    return x;
   }
   // A row's vectors of the RT heads from h0; elements of other lanes are 0.
   __device__ __forceinline__ void heads_of(const void *p, int64_t row, int64_t stride, int D,
-                                           float (&x)[RT][V]) const {
+                                           Raw<T, V> (&x)[RT]) const {
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      const auto r = ld_piece<T, V>(static_cast<const T *>(p) + row * stride + (h0 + t) * D, pc);
-      to_floats<T, V>(r, x[t]);
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (!pc.own(i) || pc.at + i >= D) x[t][i] = 0.f;
+      x[t] = ld_piece<T, V>(static_cast<const T *>(p) + row * stride + (h0 + t) * D, pc);
+      x[t].w &= mask;
     }
   }
 };
 
-// Edges of row r (0 to 0 where the offsets are out of order or out of range).
-__device__ __forceinline__ void list_of(const Attend &a, int64_t r, int64_t *start, int64_t *end) {
-  const int64_t s = a.offsets[r], e = a.offsets[r + 1];
-  const bool ok = s >= 0 && s <= e && e <= a.edges;
-  if (!ok && a.status) atomicOr(a.status, 2);
-  *start = ok ? s : 0;
-  *end = ok ? e : 0;
+// Edges of a list from its two offsets (0 to 0 where they are out of order or range).
+__device__ __forceinline__ bool list_ok(const Attend &a, int64_t s, int64_t e) {
+  return s >= 0 && s <= e && e <= a.edges;
 }
 
 // The row whose list holds edge e, found by the whole wave: 64 probes a step.  -1: none.
@@ -124,74 +154,165 @@ __device__ __forceinline__ int64_t row_at(const Attend &a, int64_t e) {
   return lo < a.nq ? lo : -1;
 }
 
+// The numbers of a wave's edges, which start at edge e0: kept in shared memory where
+// there are at most CAP, so that only the rows that they name are waited for in turn.
+// Edges are counted from e0 in 32 bits.
+struct Stage {
+  int32_t index[CAP];
+  float bias[CAP];
+  int32_t place[CAP];
+};
+struct Staged {
+  const Stage *s;
+  int64_t e0;
+  bool kept;
+};
+template <bool GRAD>
+__device__ __forceinline__ Staged stage(const Attend &a, Stage *s, int64_t e0, int64_t end) {
+  const int lane = threadIdx.x & 63;
+  const Staged g = {s, e0, end - e0 <= CAP};
+  if (!g.kept || end == e0) return g;
+  const int n = (int)(end - e0);
+  const bool bias = a.bias && a.bias_heads == 1;
+  __builtin_amdgcn_wave_barrier();
+  int32_t j[CAP / 64], to[CAP / 64];
+  float b[CAP / 64];
+#pragma unroll
+  for (int r = 0; r < CAP / 64; ++r) {
+    const int64_t i = e0 + min(r * 64 + lane, n - 1);
+    j[r] = a.indices[i];
+    if (GRAD) to[r] = a.place[i];
+  }
+  if (bias) {
+#pragma unroll
+    for (int r = 0; r < CAP / 64; ++r) b[r] = a.bias[e0 + min(r * 64 + lane, n - 1)];
+  }
+#pragma unroll
+  for (int r = 0; r < CAP / 64; ++r) {
+    const int i = r * 64 + lane;
+    s->index[i] = j[r];
+    if (bias) s->bias[i] = b[r];
+    if (GRAD) s->place[i] = to[r];
+  }
+  __builtin_amdgcn_wave_barrier();
+  return g;
+}
+
 // The part of a list that one wave reads at a time: U edges of each edge slot.
 template <typename T, int V, int RT, int U>
 struct Edges {
   Raw<T, V> k[U], v[U];
   float b[U][RT];
+  int32_t to[U];
   bool in[U], ok[U];
-  int64_t e[U];
-  __device__ __forceinline__ void load(const Attend &a, const Lane<T, V, RT> &ln, int64_t base,
-                                       int64_t end, int lg_e, bool *bad) {
+  int e[U];
+  // base: the same in a row slot; edges from `end` on are none.
+  template <bool GRAD>
+  __device__ __forceinline__ void load(const Attend &a, const Lane<T, V, RT> &ln, const Staged &g,
+                                       int base, int end, int lg_e, bool *bad) {
     int32_t j[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      e[u] = base + ((int64_t)u << lg_e) + ln.es;
+      e[u] = base + (u << lg_e) + ln.es;
       in[u] = e[u] < end;
-      j[u] = a.indices[min(e[u], a.edges - 1)];
+    }
+    const int32_t *index = a.indices + g.e0, *place = a.place + g.e0;
+    if (g.kept) {  // the same for the wave
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        j[u] = g.s->index[in[u] ? e[u] : 0];
+        if (GRAD) to[u] = g.s->place[in[u] ? e[u] : 0];
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        j[u] = index[in[u] ? e[u] : 0];
+        if (GRAD) to[u] = place[in[u] ? e[u] : 0];
+      }
+      // (keeps the two ways apart: one load for both would go by the slower generic
+      // address)
+#pragma unroll
+      for (int u = 0; u < U; ++u) asm("" : "+v"(j[u]));
+      if (GRAD) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) asm("" : "+v"(to[u]));
+      }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      ok[u] = in[u] && j[u] >= 0 && (int64_t)j[u] < a.nkv;
+      ok[u] = in[u] && (uint32_t)j[u] < (uint32_t)a.nkv;
       *bad |= in[u] && !ok[u] && j[u] != -1;
-      const int64_t row = ok[u] ? j[u] : 0;
-      k[u] = ld_piece<T, V>(static_cast<const T *>(a.k) + row * a.k_stride + ln.kvh * a.D, ln.pc);
-      v[u] = ld_piece<T, V>(static_cast<const T *>(a.v) + row * a.v_stride + ln.kvh * a.D, ln.pc);
+      const uint32_t row = ok[u] ? (uint32_t)j[u] : 0u;
+      k[u] = ld_raw<T, V>((const T *)(ln.k + (uint64_t)row * a.k_bytes));
+      v[u] = ld_raw<T, V>((const T *)(ln.v + (uint64_t)row * a.v_bytes));
     }
-    if (a.bias) {
+    if (a.bias && a.bias_heads == 1 && g.kept) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        b[u][0] = g.s->bias[in[u] ? e[u] : 0];
+#pragma unroll
+        for (int t = 1; t < RT; ++t) b[u][t] = b[u][0];
+      }
+    } else if (a.bias) {
+      const float *bias = a.bias + g.e0 * a.bias_heads + (a.bias_heads > 1 ? ln.h0 : 0);
+      const int step = a.bias_heads > 1;
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int t = 0; t < RT; ++t)
-          b[u][t] = a.bias[min(e[u], a.edges - 1) * a.bias_heads +
-                           (a.bias_heads > 1 ? ln.h0 + t : 0)];
-    }
-  }
-  // A key's (or value's) vector; foreign elements, which meet zeros, may not be infinite.
-  __device__ __forceinline__ void floats(const Lane<T, V, RT> &ln, const Raw<T, V> &r, int D,
-                                         float (&x)[V]) const {
-    to_floats<T, V>(r, x);
-    if (ln.ragged) {
+          b[u][t] = bias[(uint64_t)(uint32_t)(in[u] ? e[u] : 0) * (uint32_t)a.bias_heads + t * step];
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (!ln.pc.own(i) || ln.pc.at + i >= D) x[i] = 0.f;
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) asm("" : "+v"(b[u][t]));
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) b[u][t] = 0.f;
     }
   }
   // Scores: -inf for no edge and for a masked one, whatever its key holds.
   __device__ __forceinline__ void scores(const Attend &a, const Lane<T, V, RT> &ln,
-                                         const float (&q)[RT][V], float (&s)[U * RT]) const {
+                                         const Raw<T, V> (&q)[RT], float (&s)[U * RT]) const {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float x[V];
-      floats(ln, k[u], a.D, x);
+      const Raw<T, V> x = ln.own(k[u]);
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        float d = q[t][0] * x[0];
-#pragma unroll
-        for (int i = 1; i < V; ++i) d += q[t][i] * x[i];
-        s[u * RT + t] = d;
-      }
+      for (int t = 0; t < RT; ++t) s[u * RT + t] = dot<T, V>(q[t], x);
     }
     group_sum(s, a.lg_g);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        const float bias = a.bias ? b[u][t] : 0.f;
-        s[u * RT + t] = ok[u] && bias != NINF ? s[u * RT + t] * a.scale + bias : NINF;
+        s[u * RT + t] = ok[u] && b[u][t] != NINF ? s[u * RT + t] * a.scale + b[u][t] : NINF;
       }
   }
 };
+
+// w x added to acc; nothing is added for a weight of 0, whatever the vector holds.
+template <typename T, int V, int RT>
+__device__ __forceinline__ void add_weighted(Raw<T, V> x, const float (&w)[RT], const bool (&some)[RT],
+                                             bool apart, float (&acc)[RT][V]) {
+  bool any = false;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) any |= some[t];
+  x.w = any ? x.w : typename Raw<T, V>::W(0);
+  float y[V];
+  to_floats<T, V>(x, y);
+  if (RT == 1 || !apart) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[t][i] += w[t] * y[i];
+  } else {  // heads may be masked apart
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[t][i] += w[t] * (some[t] ? y[i] : 0.f);
+  }
+}
 
 // ------------------------------------------------------------------ forward
 template <typename T, int V, int RT>
@@ -203,8 +324,8 @@ struct State {
 // every lane of the row has the whole result.
 template <typename T, int V, int RT, int U>
 __device__ __forceinline__ void attend_list(const Attend &a, const Lane<T, V, RT> &ln,
-                                            const float (&q)[RT][V], int64_t start, int64_t end,
-                                            int lg_e, State<T, V, RT> &st, bool *bad) {
+                                            const Raw<T, V> (&q)[RT], const Staged &g, int start,
+                                            int end, int lg_e, State<T, V, RT> &st, bool *bad) {
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     st.m[t] = NINF;
@@ -212,9 +333,9 @@ __device__ __forceinline__ void attend_list(const Attend &a, const Lane<T, V, RT
 #pragma unroll
     for (int i = 0; i < V; ++i) st.acc[t][i] = 0.f;
   }
-  for (int64_t base = start; __ballot(base < end) != 0; base += (int64_t)U << lg_e) {
+  for (int base = start; __ballot(base < end) != 0; base += U << lg_e) {
     Edges<T, V, RT, U> ed;
-    ed.load(a, ln, base, end, lg_e, bad);
+    ed.template load<false>(a, ln, g, base, end, lg_e, bad);
     float s[U * RT];
     ed.scores(a, ln, q, s);
 #pragma unroll
@@ -233,17 +354,15 @@ __device__ __forceinline__ void attend_list(const Attend &a, const Lane<T, V, RT
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float x[V];
-      to_floats<T, V>(ed.v[u], x);
+      float p[RT];
+      bool some[RT];
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        const float p = s[u * RT + t];
-        st.l[t] += p;
-        if (p != 0.f) {  // an edge of weight 0 adds nothing, whatever its value holds
-#pragma unroll
-          for (int i = 0; i < V; ++i) st.acc[t][i] += p * x[i];
-        }
+        p[t] = s[u * RT + t];
+        some[t] = p[t] != 0.f;
+        st.l[t] += p[t];
       }
+      add_weighted<T, V, RT>(ed.v[u], p, some, a.bias_heads > 1, st.acc);
     }
   }
   // the edge slots of a row
@@ -265,167 +384,219 @@ __device__ __forceinline__ void attend_list(const Attend &a, const Lane<T, V, RT
   lanes_reduce<false>(st.l, from, to, AddF());
 }
 
-template <typename T, int V, int RT, int U>
-__global__ __launch_bounds__(AT) void k_attend(Attend a) {
-  bool bad = false;
-  const int wave = threadIdx.x >> 6;
-  float q[RT][V];
-  State<T, V, RT> st;
-  if ((int64_t)blockIdx.x < a.row_blocks) {
-    const Lane<T, V, RT> ln(a, a.lg_e);
-    const int rows = 64 >> (a.lg_g + a.lg_h + a.lg_e);
-    const int64_t row = ((int64_t)blockIdx.x * AW + wave) * rows + ln.rs;
-    const bool live = row < a.nq;
-    int64_t start = 0, end = 0;
-    if (live) list_of(a, row, &start, &end);
-    const bool chunked = a.chunks && end - start > a.ch;
-    if (chunked) end = start;
-    ln.heads_of(a.q, live ? row : a.nq - 1, a.q_stride, a.D, q);
-    attend_list<T, V, RT, U>(a, ln, q, start, end, a.lg_e, st, &bad);
-    if (live && !chunked && ln.head && ln.es == 0) {
-#pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        const int h = ln.h0 + t;
-        const float inv = st.l[t] == 0.f ? 0.f : 1.f / st.l[t];
-        float y[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) y[i] = st.acc[t][i] * inv;
-        st_piece<false>(from_floats<T, V>(y),
-                        static_cast<T *>(a.out) + (row * a.heads + h) * a.D, ln.pc);
-        if ((threadIdx.x & ((1 << a.lg_g) - 1)) == 0)
-          a.lse[row * a.heads + h] = st.l[t] == 0.f ? NINF : st.m[t] + logf(st.l[t]);
-      }
-    }
+// Calls task(lane, row, start, end, staged, lg_e, slot) for each of the wave's tasks, all
+// lanes together: rounds of rows, one in each row slot (slot = -1; -2 where there is none
+// or its list is cut into chunks, and then start = end), or the long lists that reach into
+// the wave's chunk (slot: of the partial result).
+template <bool GRAD, typename LaneT, typename Task>
+__device__ __forceinline__ void take_work(const Attend &a, Stage *s, Task task) {
+  // (the same in the wave's lanes, which the compiler cannot see)
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int lane = threadIdx.x & 63;
+  const bool by_rows = (int64_t)blockIdx.x >= a.chunk_blocks;
+  const int lg_e = by_rows ? a.lg_e : 6 - a.lg_g - a.lg_h;
+  const int slots = 64 >> (a.lg_g + a.lg_h + lg_e);  // 1 for chunks
+  const int64_t unit =
+      ((int64_t)blockIdx.x - (by_rows ? a.chunk_blocks : 0)) * AW + wave;  // wave or chunk
+  int64_t r0 = 0, off, first = -1, last = -1;
+  int tasks;
+  Staged g;
+  if (by_rows) {
+    r0 = unit * slots * a.rounds;
+    if (r0 >= a.nq) return;
+    tasks = (int)min((int64_t)(slots * a.rounds), a.nq - r0);  // rows: at most 32
+    off = a.offsets[r0 + min(lane, tasks)];
+    const int64_t e0 = read_lane(off, 0), e1 = read_lane(off, tasks);
+    const bool ok = list_ok(a, e0, e1);
+    g = stage<GRAD>(a, s, ok ? e0 : 0, ok ? e1 : 0);
   } else {
-    const int lg_e = 6 - a.lg_g - a.lg_h;
-    const Lane<T, V, RT> ln(a, lg_e);
-    const int64_t c = ((int64_t)blockIdx.x - a.row_blocks) * AW + wave;
-    if (c >= a.chunks) return;
-    const int64_t lo = c * a.ch, hi = min(lo + a.ch, a.edges);
-    const int64_t r0 = row_at(a, lo), r1 = row_at(a, hi - 1);
+    if (unit >= a.chunks) return;
+    const int64_t lo = unit * a.ch, hi = min(lo + a.ch, a.edges);
+    // lanes 0 and 1: the rows that hold the chunk's first and last edge
+    first = row_at(a, lo);
+    last = row_at(a, hi - 1);
+    const int64_t mine = lane ? last : first;
+    int64_t start = 0, end = 0;
+    if (lane < 2 && mine >= 0 && !(lane && first == last)) {
+      start = a.offsets[mine];
+      end = a.offsets[mine + 1];
+    }
+    const bool cut = list_ok(a, start, end) && end - start > a.ch;
+    const uint64_t cuts = __ballot(cut), begin = __ballot(cut && start >= lo);
+    if (blockIdx.y == 0 && (begin ? (begin >> lane) & 1 : lane == 0))
+      a.starts[unit] = begin ? mine : -1;
+    if (!cuts) return;
+    tasks = 2;
+    off = cut ? max(start, lo) : lo;  // lane 0 to 3: starts and ends
+    const int64_t stop = cut ? min(end, hi) : lo;
+    const int64_t ends = __shfl(stop, lane & 1, 64);
+    off = lane < 2 ? off : ends;
+    g = stage<GRAD>(a, s, lo, hi);
+  }
+  const LaneT ln(a, lg_e);
 #pragma unroll 1
-    for (int side = 0; side < 2; ++side) {
-      const int64_t row = side ? r1 : r0;
-      if (row < 0 || (side && r1 == r0)) continue;  // the same for the wave
-      int64_t start, end;
-      list_of(a, row, &start, &end);
-      if (end - start <= a.ch) continue;
-      ln.heads_of(a.q, row, a.q_stride, a.D, q);
-      attend_list<T, V, RT, U>(a, ln, q, max(start, lo), min(end, hi), lg_e, st, &bad);
-      if (ln.head && ln.es == 0) {
-        float *part = a.part + (2 * c + side) * a.slot;
+  for (int i = 0; i * slots < tasks; ++i) {
+    const int at = i * slots + ln.rs;
+    int64_t start = __shfl(off, at & 63, 64);
+    int64_t end = __shfl(off, (by_rows ? at + 1 : at + 2) & 63, 64);
+    int64_t row, slot = -2;
+    if (by_rows) {
+      const bool there = at < tasks;
+      const bool ok = list_ok(a, start, end) && start >= g.e0;
+      if (there && !ok && a.status) atomicOr(a.status, 2);
+      if (!ok) end = start;
+      if (there && !(a.chunks && end - start > a.ch)) slot = -1;
+      row = there ? r0 + at : r0;
+    } else {
+      if (__ballot(start < end) == 0) continue;
+      row = i ? last : first;
+      slot = 2 * unit + i;
+    }
+    if (slot == -2 || start >= end) start = end = g.e0;
+    task(ln, row, (int)(start - g.e0), (int)(end - g.e0), g, lg_e, slot);
+  }
+}
+
+template <typename T, int V, int RT, int U>
+__global__ __launch_bounds__(AT, RT == 4 ? 2 : RT == 2 ? 3 : 4) void k_attend(Attend a) {
+  __shared__ Stage s_stage[AW];
+  typedef Lane<T, V, RT> L;
+  bool bad = false;
+  take_work<false, L>(
+      a, &s_stage[__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))],
+      [&](const L &ln, int64_t row, int start, int end, const Staged &g, int lg_e, int64_t slot) {
+        Raw<T, V> q[RT];
+        State<T, V, RT> st;
+        ln.heads_of(a.q, row, a.q_stride, a.D, q);
+        attend_list<T, V, RT, U>(a, ln, q, g, start, end, lg_e, st, &bad);
+        if (slot == -2 || !ln.head || ln.es) return;
+        float *part = a.part + slot * a.slot;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           const int h = ln.h0 + t;
-          Raw<float, V> r;
-          memcpy(&r.w, st.acc[t], sizeof(st.acc[t]));
-          st_piece<false>(r, part + h * a.D, ln.pc);
-          if ((threadIdx.x & ((1 << a.lg_g) - 1)) == 0) {
-            part[a.heads * a.D + 2 * h] = st.m[t];
-            part[a.heads * a.D + 2 * h + 1] = st.l[t];
+          if (slot >= 0) {
+            Raw<float, V> r;
+            memcpy(&r.w, st.acc[t], sizeof(st.acc[t]));
+            st_piece<false>(r, part + h * a.D, ln.pc);
+            if (ln.first) {
+              part[a.heads * a.D + 2 * h] = st.m[t];
+              part[a.heads * a.D + 2 * h + 1] = st.l[t];
+            }
+            continue;
           }
+          const float inv = st.l[t] == 0.f ? 0.f : 1.f / st.l[t];
+          float y[V];
+#pragma unroll
+          for (int i = 0; i < V; ++i) y[i] = st.acc[t][i] * inv;
+          st_piece<false>(from_floats<T, V>(y),
+                          static_cast<T *>(a.out) + (row * a.heads + h) * a.D, ln.pc);
+          if (ln.first)
+            a.lse[row * a.heads + h] = st.l[t] == 0.f ? NINF : st.m[t] + logf(st.l[t]);
         }
-      }
-    }
-  }
+      });
   if (bad && a.status) atomicOr(a.status, 1);
 }
 
-// A block per chunk and head; where a long list starts in the chunk, it joins the list's
-// partial results: 1024 / 2^lg groups of lanes take every such part, a column each.
+// Joins the partial results of the long lists, a list at a time: groups of 2^lg lanes take
+// every such part, C columns a lane.  A block looks through 64 chunks for those in which a
+// list starts, so that a call without long lists pays for few blocks.
 constexpr int JT = 1024;
-struct LongList {
-  int64_t row, first, parts;  // the first part's slot; the others are 2 (c + 1), 2 (c + 2), ..
-};
-__device__ __forceinline__ LongList long_list(const Attend &a, int64_t c) {
-  LongList l = {-1, 0, 0};
-  const int64_t lo = c * a.ch, hi = min(lo + a.ch, a.edges);
-  const int64_t row = row_at(a, hi - 1);
-  if (row < 0) return l;
-  const int64_t start = a.offsets[row], end = a.offsets[row + 1];
-  if (start < lo || end > a.edges || end - start <= a.ch) return l;
-  l.row = row;
-  l.first = 2 * c + (start > lo);
-  l.parts = (end - 1) / a.ch - c + 1;
-  return l;
-}
-
-template <typename T, bool GRAD>
+template <typename T, bool GRAD, int C>
 __global__ __launch_bounds__(JT) void k_attend_join(Attend a, int lg) {
-  __shared__ float s_m[JT / 64], s_acc[JT], s_l[JT];
-  const int64_t c = blockIdx.x;
+  __shared__ float s_m[JT / 64], s_acc[C][JT], s_l[JT];
   const int h = blockIdx.y;
-  const LongList l = long_list(a, c);
-  if (l.row < 0) return;  // the same for the block
-  const int d = threadIdx.x & ((1 << lg) - 1), g = threadIdx.x >> lg, groups = JT >> lg;
-  auto part = [&](int64_t j) { return a.part + (j ? 2 * (c + j) : l.first) * a.slot; };
-  float top = NINF, from = 0.f;
-  if (!GRAD) {
-    for (int64_t j = threadIdx.x; j < l.parts; j += JT)
-      top = fmaxf(top, part(j)[a.heads * a.D + 2 * h]);
-    float t[1] = {top};
-    lanes_reduce<true>(t, 0, 6, MaxF());
-    if ((threadIdx.x & 63) == 0) s_m[threadIdx.x >> 6] = t[0];
-    __syncthreads();
-    top = NINF;
+  const int d = (threadIdx.x & ((1 << lg) - 1)) * C, g = threadIdx.x >> lg, groups = JT >> lg;
+  const int64_t c0 = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+  uint64_t todo = __ballot(c0 < a.chunks && a.starts[min(c0, a.chunks - 1)] >= 0);
+  while (todo) {  // the same for the block
+    const int64_t c = (int64_t)blockIdx.x * 64 + __builtin_ctzll(todo);
+    todo &= todo - 1;
+    const int64_t row = a.starts[c];
+    const int64_t start = a.offsets[row], end = a.offsets[row + 1];
+    const int64_t first = 2 * c + (start > c * a.ch), parts = (end - 1) / a.ch - c + 1;
+    auto part = [&](int64_t j) { return a.part + (j ? 2 * (c + j) : first) * a.slot; };
+    float top = NINF, from = 0.f;
+    if (!GRAD) {
+      for (int64_t j = threadIdx.x; j < parts; j += JT)
+        top = fmaxf(top, part(j)[a.heads * a.D + 2 * h]);
+      float t[1] = {top};
+      lanes_reduce<true>(t, 0, 6, MaxF());
+      if ((threadIdx.x & 63) == 0) s_m[threadIdx.x >> 6] = t[0];
+      __syncthreads();
+      top = NINF;
 #pragma unroll
-    for (int i = 0; i < JT / 64; ++i) top = fmaxf(top, s_m[i]);
-    from = top == NINF ? 0.f : top;
-  }
-  float acc = 0.f, sum = 0.f;
-  for (int64_t j0 = g; j0 < l.parts; j0 += 8 * groups) {
-    float x[8], m[8], ls[8];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const float *p = part(min(j0 + u * groups, l.parts - 1));
-      x[u] = p[h * a.D + min(d, a.D - 1)];
-      m[u] = GRAD ? 0.f : p[a.heads * a.D + 2 * h];
-      ls[u] = GRAD ? 0.f : p[a.heads * a.D + 2 * h + 1];
+      for (int i = 0; i < JT / 64; ++i) top = fmaxf(top, s_m[i]);
+      from = top == NINF ? 0.f : top;
     }
+    float acc[C] = {}, sum = 0.f;
+    for (int64_t j0 = g; j0 < parts; j0 += 8 * groups) {
+      Raw<float, C> x[8];
+      float m[8], ls[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      if (j0 + u * groups >= l.parts) continue;
-      const float f = GRAD ? 1.f : exp_of(m[u] - from);
-      if (f != 0.f) {
-        acc += f * x[u];
-        sum += f * ls[u];
+      for (int u = 0; u < 8; ++u) {
+        const float *p = part(min(j0 + u * groups, parts - 1));
+        x[u] = ld_raw<float, C>(p + h * a.D + min(d, a.D - C));
+        m[u] = GRAD ? 0.f : p[a.heads * a.D + 2 * h];
+        ls[u] = GRAD ? 0.f : p[a.heads * a.D + 2 * h + 1];
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        if (j0 + u * groups >= parts) continue;
+        const float f = GRAD ? 1.f : exp_of(m[u] - from);
+        if (f != 0.f) {
+          float y[C];
+          to_floats<float, C>(x[u], y);
+#pragma unroll
+          for (int i = 0; i < C; ++i) acc[i] += f * y[i];
+          sum += f * ls[u];
+        }
       }
     }
-  }
-  s_acc[threadIdx.x] = acc;
-  s_l[threadIdx.x] = sum;
-  __syncthreads();
-  if (g != 0 || d >= a.D) return;
-  acc = sum = 0.f;
-  for (int i = 0; i < groups; ++i) {
-    acc += s_acc[(i << lg) + d];
-    sum += s_l[(i << lg) + d];
-  }
-  const int64_t at = (l.row * a.heads + h) * a.D + d;
-  if (GRAD) {
-    static_cast<T *>(a.dq)[at] = (T)(acc * a.scale);
-  } else {
-    static_cast<T *>(a.out)[at] = (T)(sum == 0.f ? 0.f : acc / sum);
-    if (d == 0) a.lse[l.row * a.heads + h] = sum == 0.f ? NINF : top + logf(sum);
+#pragma unroll
+    for (int i = 0; i < C; ++i) s_acc[i][threadIdx.x] = acc[i];
+    s_l[threadIdx.x] = sum;
+    __syncthreads();
+    // halves of the groups, in the same order each time
+    for (int n = groups >> 1; n > 0; n >>= 1) {
+      if (g < n) {
+        const int other = threadIdx.x + (n << lg);
+#pragma unroll
+        for (int i = 0; i < C; ++i) s_acc[i][threadIdx.x] += s_acc[i][other];
+        s_l[threadIdx.x] += s_l[other];
+      }
+      __syncthreads();
+    }
+    if (g == 0 && d < a.D) {
+      sum = s_l[threadIdx.x];
+      const int64_t at = (row * a.heads + h) * a.D + d;
+      float y[C];
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        const float x = s_acc[i][threadIdx.x];
+        y[i] = GRAD ? x * a.scale : sum == 0.f ? 0.f : x / sum;
+      }
+      st_raw<false>(from_floats<T, C>(y), static_cast<T *>(GRAD ? a.dq : a.out) + at);
+      if (!GRAD && d == 0) a.lse[row * a.heads + h] = sum == 0.f ? NINF : top + logf(sum);
+    }
+    __syncthreads();
   }
 }
 
 // ------------------------------------------------------------------ gradient by rows
 template <typename T, int V, int RT, int U>
 __device__ __forceinline__ void grad_list(const Attend &a, const Lane<T, V, RT> &ln, int64_t row,
-                                          int64_t start, int64_t end, int lg_e,
+                                          const Staged &g, int start, int end, int lg_e,
                                           float (&dq)[RT][V], bool *bad) {
-  float q[RT][V], go[RT][V], delta[RT], lse[RT];
+  Raw<T, V> q[RT], go[RT];
+  float delta[RT], lse[RT];
   ln.heads_of(a.q, row, a.q_stride, a.D, q);
   ln.heads_of(a.go, row, a.go_stride, a.D, go);
   {
-    float o[RT][V];
+    Raw<T, V> o[RT];
     ln.heads_of(a.o, row, a.o_stride, a.D, o);
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      delta[t] = 0.f;
-#pragma unroll
-      for (int i = 0; i < V; ++i) delta[t] += go[t][i] * o[t][i];
+      delta[t] = dot<T, V>(go[t], o[t]);
       lse[t] = a.lse_in[row * a.heads + ln.h0 + t];
     }
   }
@@ -434,41 +605,44 @@ __device__ __forceinline__ void grad_list(const Attend &a, const Lane<T, V, RT> 
   for (int t = 0; t < RT; ++t)
 #pragma unroll
     for (int i = 0; i < V; ++i) dq[t][i] = 0.f;
-  const bool writer = ln.head && (threadIdx.x & ((1 << a.lg_g) - 1)) == 0;
-  for (int64_t base = start; __ballot(base < end) != 0; base += (int64_t)U << lg_e) {
+  for (int base = start; __ballot(base < end) != 0; base += U << lg_e) {
     Edges<T, V, RT, U> ed;
-    ed.load(a, ln, base, end, lg_e, bad);
+    ed.template load<true>(a, ln, g, base, end, lg_e, bad);
     float s[U * RT], dp[U * RT];
     ed.scores(a, ln, q, s);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float x[V];
-      ed.floats(ln, ed.v[u], a.D, x);
+      const Raw<T, V> x = ln.own(ed.v[u]);
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        float d = go[t][0] * x[0];
-#pragma unroll
-        for (int i = 1; i < V; ++i) d += go[t][i] * x[i];
-        dp[u * RT + t] = d;
-      }
+      for (int t = 0; t < RT; ++t) dp[u * RT + t] = dot<T, V>(go[t], x);
     }
     group_sum(dp, a.lg_g);
+    float sum[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float x[V];
-      to_floats<T, V>(ed.k[u], x);
+      float ds[RT];
+      bool some[RT];
+      sum[u] = 0.f;
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         // a row without weight has lse = -inf and no gradient
         const float p = lse[t] == NINF ? 0.f : exp_of(s[u * RT + t] - lse[t]);
-        const float ds = p == 0.f ? 0.f : p * (dp[u * RT + t] - delta[t]);
-        if (p != 0.f) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) dq[t][i] += ds * x[i];
-        }
-        if (writer && ed.in[u]) a.pd[ed.e[u] * a.heads + ln.h0 + t] = float2{p, ds};
+        some[t] = p != 0.f;
+        ds[t] = some[t] ? p * (dp[u * RT + t] - delta[t]) : 0.f;
+        sum[u] += ds[t];
+        if (ln.first && ln.head && ed.in[u]) a.pd[(int64_t)ed.to[u] * a.heads + ln.h0 + t] = float2{p, ds[t]};
+        if (a.db && a.bias_heads > 1 && ln.first && ln.head && ed.in[u])
+          a.db[(g.e0 + ed.e[u]) * a.bias_heads + ln.h0 + t] = ds[t];
       }
-      if (writer && ln.kvh == 0 && ln.h0 == 0 && ed.in[u]) a.row_of[ed.e[u]] = (int32_t)row;
+      add_weighted<T, V, RT>(ed.k[u], ds, some, a.bias_heads > 1, dq);
+      if (ln.first && ln.head && ln.h0 == 0 && ed.in[u]) a.row_of[ed.to[u]] = (int32_t)row;
+      if (!ln.head) sum[u] = 0.f;
+    }
+    if (a.db && a.bias_heads == 1) {  // all heads are in the wave (else k_attend_grad_bias)
+      lanes_reduce<false>(sum, a.lg_g, a.lg_g + a.lg_h, AddF());
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (ln.first && ln.h0 == 0 && ln.head && ed.in[u]) a.db[g.e0 + ed.e[u]] = sum[u];
     }
   }
   const int from = a.lg_g + a.lg_h;
@@ -477,67 +651,46 @@ __device__ __forceinline__ void grad_list(const Attend &a, const Lane<T, V, RT> 
 }
 
 template <typename T, int V, int RT, int U>
-__global__ __launch_bounds__(AT) void k_attend_grad_rows(Attend a) {
+__global__ __launch_bounds__(AT, RT == 4 ? 2 : RT == 2 ? 3 : 4) void k_attend_grad_rows(Attend a) {
+  __shared__ Stage s_stage[AW];
+  typedef Lane<T, V, RT> L;
   bool bad = false;
-  const int wave = threadIdx.x >> 6;
-  float dq[RT][V];
-  if ((int64_t)blockIdx.x < a.row_blocks) {
-    const Lane<T, V, RT> ln(a, a.lg_e);
-    const int rows = 64 >> (a.lg_g + a.lg_h + a.lg_e);
-    const int64_t row = ((int64_t)blockIdx.x * AW + wave) * rows + ln.rs;
-    const bool live = row < a.nq;
-    int64_t start = 0, end = 0;
-    if (live) list_of(a, row, &start, &end);
-    const bool chunked = a.chunks && end - start > a.ch;
-    if (chunked) end = start;
-    grad_list<T, V, RT, U>(a, ln, live ? row : a.nq - 1, start, end, a.lg_e, dq, &bad);
-    if (live && !chunked && ln.head && ln.es == 0) {
-#pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        float y[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) y[i] = dq[t][i] * a.scale;
-        st_piece<false>(from_floats<T, V>(y),
-                        static_cast<T *>(a.dq) + (row * a.heads + ln.h0 + t) * a.D, ln.pc);
-      }
-    }
-  } else {
-    const int lg_e = 6 - a.lg_g - a.lg_h;
-    const Lane<T, V, RT> ln(a, lg_e);
-    const int64_t c = ((int64_t)blockIdx.x - a.row_blocks) * AW + wave;
-    if (c >= a.chunks) return;
-    const int64_t lo = c * a.ch, hi = min(lo + a.ch, a.edges);
-    const int64_t r0 = row_at(a, lo), r1 = row_at(a, hi - 1);
-#pragma unroll 1
-    for (int side = 0; side < 2; ++side) {
-      const int64_t row = side ? r1 : r0;
-      if (row < 0 || (side && r1 == r0)) continue;  // the same for the wave
-      int64_t start, end;
-      list_of(a, row, &start, &end);
-      if (end - start <= a.ch) continue;
-      grad_list<T, V, RT, U>(a, ln, row, max(start, lo), min(end, hi), lg_e, dq, &bad);
-      if (ln.head && ln.es == 0) {
+  take_work<true, L>(
+      a, &s_stage[__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))],
+      [&](const L &ln, int64_t row, int start, int end, const Staged &g, int lg_e, int64_t slot) {
+        float dq[RT][V];
+        grad_list<T, V, RT, U>(a, ln, row, g, start, end, lg_e, dq, &bad);
+        if (slot == -2 || !ln.head || ln.es) return;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-          Raw<float, V> r;
-          memcpy(&r.w, dq[t], sizeof(dq[t]));
-          st_piece<false>(r, a.part + (2 * c + side) * a.slot + (ln.h0 + t) * a.D, ln.pc);
+          if (slot >= 0) {
+            Raw<float, V> r;
+            memcpy(&r.w, dq[t], sizeof(dq[t]));
+            st_piece<false>(r, a.part + slot * a.slot + (ln.h0 + t) * a.D, ln.pc);
+            continue;
+          }
+          float y[V];
+#pragma unroll
+          for (int i = 0; i < V; ++i) y[i] = dq[t][i] * a.scale;
+          st_piece<false>(from_floats<T, V>(y),
+                          static_cast<T *>(a.dq) + (row * a.heads + ln.h0 + t) * a.D, ln.pc);
         }
-      }
-    }
-  }
+      });
   if (bad && a.status) atomicOr(a.status, 1);
 }
 
 // ------------------------------------------------------------------ gradient by keys
 // A group of 2^lg lanes per chunk of the edges in the order of their keys, each lane a
 // vector of one key head (vph vectors per head); blocks from sum_blocks on write the
-// rows of keys without an edge as zeros.
+// rows of keys without an edge as zeros.  The steps are the edges' query heads: `share`
+// for each edge, U of them in flight.
 template <typename T, int V>
 __global__ __launch_bounds__(AT) void k_attend_grad_keys(Attend a, IdSort so, T *dk, T *dv, int vph,
-                                                         int lg, int64_t sum_blocks) {
+                                                         int64_t sum_blocks) {
   constexpr int U = 4;
-  const int sub = threadIdx.x & ((1 << lg) - 1), per = AT >> lg;
+  extern __shared__ int2 s_entries[];
+  const int lg = so.lg, sub = threadIdx.x & ((1 << lg) - 1), g = threadIdx.x >> lg;
+  const int per = AT >> lg;
   const int at = (blockIdx.y << lg) + sub;
   const int kvh = min(at / vph, a.kv_heads - 1);
   const Piece<V> pc(at < a.kv_heads * vph ? at - kvh * vph : vph, a.D);
@@ -545,120 +698,73 @@ __global__ __launch_bounds__(AT) void k_attend_grad_keys(Attend a, IdSort so, T 
   if ((int64_t)blockIdx.x >= sum_blocks) {
     const int64_t groups = ((int64_t)gridDim.x - sum_blocks) * per;
     const float zero[V] = {};
-    for (int64_t r = ((int64_t)blockIdx.x - sum_blocks) * per + (threadIdx.x >> lg); r < a.nkv;
-         r += groups) {
+    for (int64_t r = ((int64_t)blockIdx.x - sum_blocks) * per + g; r < a.nkv; r += groups) {
       if (so.seen[r]) continue;
       st_piece<false>(from_floats<T, V>(zero), dk + r * width + kvh * a.D, pc);
       st_piece<false>(from_floats<T, V>(zero), dv + r * width + kvh * a.D, pc);
     }
     return;
   }
-  const int64_t c = (int64_t)blockIdx.x * per + (threadIdx.x >> lg);
+  const int64_t c = (int64_t)blockIdx.x * per + g;
   if (c >= so.chunks) return;
   const uint32_t limit = (uint32_t)a.nkv;
-  const Chunk k = chunk_of(so.dst, so.n, so.C, c);
-  const int64_t end = k.beyond ? min(k.stop + so.C, so.n) : k.stop;
-  float ak[V], av[V];
-  int32_t cur = -1;
-  bool lead = k.lead_part;
-  auto flush = [&](bool final) {
-    if ((uint32_t)cur >= limit) return;
-    if (lead || (final && k.trail_part)) {
-      float *p = so.part + (2 * c + (lead ? 0 : 1)) * so.width + kvh * a.D;
-      Raw<float, V> r;
-      memcpy(&r.w, ak, sizeof(ak));
-      st_piece<false>(r, p, pc);
-      memcpy(&r.w, av, sizeof(av));
-      st_piece<false>(r, p + width, pc);
-      if (!lead && sub == 0 && blockIdx.y == 0) so.long_at[atomicAdd(so.n_long, 1)] = (int32_t)c;
-    } else {
-      float y[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) y[i] = ak[i] * a.scale;
-      st_piece<false>(from_floats<T, V>(y), dk + cur * width + kvh * a.D, pc);
-      st_piece<false>(from_floats<T, V>(av), dv + cur * width + kvh * a.D, pc);
-    }
-    lead = false;
-  };
-  bool done = false;
-  for (int64_t i = k.begin; i < end && !done; i += U) {
-    int32_t d[U], e[U], row[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t j = min(i + u, so.n - 1);
-      d[u] = so.dst[j];
-      e[u] = so.order[j];
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) row[u] = a.row_of[e[u]];
-    float xk[U][V], xv[U][V];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int x = 0; x < V; ++x) xk[u][x] = xv[u][x] = 0.f;
-    for (int t = 0; t < a.share; ++t) {
-      const int h = kvh * a.share + t;
-      Raw<T, V> rq[U], rg[U];
-      float2 w[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        // (an edge of no row: its weights were not written)
-        const bool ok = (uint32_t)d[u] < limit && (uint32_t)row[u] < (uint32_t)a.nq;
-        const int64_t r = ok ? row[u] : 0;
-        w[u] = a.pd[(int64_t)e[u] * a.heads + h];
+  const float2 *pd = a.pd + kvh * a.share;
+  const T *q = static_cast<const T *>(a.q) + kvh * a.share * a.D + pc.at;
+  const T *go = static_cast<const T *>(a.go) + kvh * a.share * a.D + pc.at;
+  float ak[V] = {}, av[V] = {};
+  float2 w[U];
+  Raw<T, V> rq[U], rg[U];
+  walk_chunk<U>(
+      so, a.row_of, limit, a.share, lg, c, s_entries + g * so.C,
+      [&](int u, int64_t i, int32_t row, int t, bool ok) {
+        ok = ok && (uint32_t)row < (uint32_t)a.nq;  // (an edge of no row: no weights are there)
+        const int64_t r = ok ? row : 0;
+        w[u] = pd[i * a.heads + t];
+        rq[u] = ld_raw<T, V>(q + r * a.q_stride + t * a.D);
+        rg[u] = ld_raw<T, V>(go + r * a.go_stride + t * a.D);
         if (!ok) w[u] = float2{0.f, 0.f};
-        rq[u] = ld_piece<T, V>(static_cast<const T *>(a.q) + r * a.q_stride + h * a.D, pc);
-        rg[u] = ld_piece<T, V>(static_cast<const T *>(a.go) + r * a.go_stride + h * a.D, pc);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
+      },
+      [&](int u) {
+        // an edge of weight 0 adds nothing, whatever its row holds
+        const bool some = w[u].x != 0.f;
+        rq[u].w = some ? rq[u].w : typename Raw<T, V>::W(0);
+        rg[u].w = some ? rg[u].w : typename Raw<T, V>::W(0);
         float y[V];
-        if (w[u].x != 0.f) {
-          to_floats<T, V>(rq[u], y);
+        to_floats<T, V>(rq[u], y);
 #pragma unroll
-          for (int x = 0; x < V; ++x) xk[u][x] += w[u].y * y[x];
-          to_floats<T, V>(rg[u], y);
+        for (int i = 0; i < V; ++i) ak[i] += w[u].y * y[i];
+        to_floats<T, V>(rg[u], y);
 #pragma unroll
-          for (int x = 0; x < V; ++x) xv[u][x] += w[u].x * y[x];
+        for (int i = 0; i < V; ++i) av[i] += w[u].x * y[i];
+      },
+      [&](int32_t node, int part) {
+        if ((uint32_t)node < limit && part < 2) {
+          float *p = so.part + (2 * c + part) * so.width + kvh * a.D;
+          Raw<float, V> r;
+          memcpy(&r.w, ak, sizeof(ak));
+          st_piece<false>(r, p, pc);
+          memcpy(&r.w, av, sizeof(av));
+          st_piece<false>(r, p + width, pc);
+          if (part && sub == 0 && blockIdx.y == 0)
+            so.long_at[atomicAdd(so.n_long, 1)] = LongAt{(int32_t)c, node};
+        } else if ((uint32_t)node < limit) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) ak[i] *= a.scale;
+          st_piece<true>(from_floats<T, V>(ak), dk + node * width + kvh * a.D, pc);
+          st_piece<true>(from_floats<T, V>(av), dv + node * width + kvh * a.D, pc);
         }
-      }
-    }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (done || i + u >= end || (i + u >= k.stop && d[u] != k.last)) {
-        done = true;
-        continue;
-      }
-      if (i + u == k.begin || d[u] != cur) {
-        if (i + u != k.begin) flush(false);
-        cur = d[u];
-#pragma unroll
-        for (int x = 0; x < V; ++x) {
-          ak[x] = xk[u][x];
-          av[x] = xv[u][x];
-        }
-      } else {
-#pragma unroll
-        for (int x = 0; x < V; ++x) {
-          ak[x] += xk[u][x];
-          av[x] += xv[u][x];
-        }
-      }
-    }
-  }
-  if (k.begin < end) flush(true);
+        for (int i = 0; i < V; ++i) ak[i] = av[i] = 0.f;
+      });
 }
 
-// db: ds of the edge's heads, added up where they share the bias.
+// db where the heads share a bias and no wave has them all.
 __global__ __launch_bounds__(AT) void k_attend_grad_bias(Attend a, float *db) {
-  const int64_t n = a.edges * a.bias_heads;
-  for (int64_t i = (int64_t)blockIdx.x * AT + threadIdx.x; i < n; i += (int64_t)gridDim.x * AT) {
-    if (a.bias_heads > 1) {
-      db[i] = a.pd[i].y;
-      continue;
-    }
+  for (int64_t i = (int64_t)blockIdx.x * AT + threadIdx.x; i < a.edges;
+       i += (int64_t)gridDim.x * AT) {
+    const float2 *p = a.pd + (int64_t)a.place[i] * a.heads;
     float t = 0.f;
-    for (int h = 0; h < a.heads; ++h) t += a.pd[i * a.heads + h].y;
+    for (int h = 0; h < a.heads; ++h) t += p[h].y;
     db[i] = t;
   }
 }
@@ -678,20 +784,26 @@ void fill_rows(T *p, int64_t n, float value, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------ host side
-// Chunk length: about 2048 chunks, of 128 to 1024 edges.
-int chunk_edges(int64_t edges) {
-  int ch = 128;
-  while (ch < 1024 && edges > (int64_t)ch * 2048) ch *= 2;
-  return ch;
-}
+// Edges of a chunk: as many as a wave keeps in shared memory, half as many where those
+// would leave compute units without a wave.
+int chunk_edges(int64_t edges) { return edges > (1 << 19) ? CAP : CAP / 2; }
 // Chunks of lists of up to `edges` edges, which never shrinks with the number.
 int64_t most_chunks(int64_t edges) {
-  const int64_t c = (edges + 1023) / 1024, few = (edges + 127) / 128;
-  return few <= 2048 ? few : c > 2048 ? c : 2048;
+  const int64_t few = (edges + CAP / 2 - 1) / (CAP / 2), c = (edges + CAP - 1) / CAP;
+  return few <= (1 << 19) / (CAP / 2) ? few : std::max(c, (int64_t)(1 << 19) / (CAP / 2));
 }
+// The partial results and the rows that the chunks note.
 size_t part_bytes(int64_t edges, int64_t slot) {
-  if (edges <= chunk_edges(edges)) return 256;
-  return ((size_t)(2 * most_chunks(edges)) * (size_t)slot * sizeof(float) + 255) & ~(size_t)255;
+  if (edges <= CAP / 2) return 256;
+  Carve c(nullptr);
+  c.take<float>((size_t)(2 * most_chunks(edges) * slot));
+  c.take<int64_t>((size_t)most_chunks(edges));
+  return c.used;
+}
+void set_parts(Attend &a, void *p) {
+  Carve c(p);
+  a.part = c.take<float>((size_t)(2 * most_chunks(a.edges) * a.slot));
+  a.starts = c.take<int64_t>((size_t)most_chunks(a.edges));
 }
 
 void set_lanes(Attend &a, int vec) {
@@ -702,11 +814,18 @@ void set_lanes(Attend &a, int vec) {
   // edge slots for a list of middling length in one round of four edges a slot
   const int want = log2_up((a.edges / a.nq + 3) / 4);
   a.lg_e = want < rest ? want : rest;
-  const int rows = AW * (64 >> (a.lg_g + a.lg_h + a.lg_e));
-  a.row_blocks = (a.nq + rows - 1) / rows;
+  const int slots = 64 >> (a.lg_g + a.lg_h + a.lg_e);
+  // rows one after the other while the waves fill the chip, and their edges fit a stage
+  a.rounds = 1;
+  while (a.rounds < 4 && slots * a.rounds < 32 && a.nq > (int64_t)slots * a.rounds * 2 * 8192 &&
+         a.edges / a.nq * slots * a.rounds < CAP / 2)
+    a.rounds *= 2;
   a.ch = chunk_edges(a.edges);
   a.chunks = a.edges > a.ch ? (a.edges + a.ch - 1) / a.ch : 0;
+  a.chunk_blocks = (a.chunks + AW - 1) / AW;
 }
+// Whether each wave has all heads.
+bool heads_in_wave(const Attend &a, int rt) { return a.kv_heads <= 1 << a.lg_h && a.share == rt; }
 
 // Calls f(RT, U) with the query heads that a wave takes of each key head and the edges in
 // flight per lane.
@@ -719,12 +838,23 @@ void with_heads(int share, F f) {
 }
 dim3 attend_grid(const Attend &a, int rt) {
   const int tiles = (a.kv_heads + (1 << a.lg_h) - 1) >> a.lg_h;
-  return dim3((unsigned)(a.row_blocks + (a.chunks + AW - 1) / AW),
+  const int64_t rows = (int64_t)AW * (64 >> (a.lg_g + a.lg_h + a.lg_e)) * a.rounds;
+  return dim3((unsigned)(a.chunk_blocks + (a.nq + rows - 1) / rows),
               (unsigned)(tiles * (a.share / rt)));
+}
+template <typename T, bool GRAD>
+void launch_join(const Attend &a, hipStream_t s) {
+  if (!a.chunks) return;
+  const dim3 g((unsigned)((a.chunks + 63) / 64), (unsigned)a.heads);
+  if (a.D % 4 == 0)
+    hipLaunchKernelGGL((k_attend_join<T, GRAD, 4>), g, dim3(JT), 0, s, a, log2_up(a.D / 4));
+  else
+    hipLaunchKernelGGL((k_attend_join<T, GRAD, 1>), g, dim3(JT), 0, s, a, log2_up(a.D));
 }
 
 int check_attend(const char *who, int64_t nq, int64_t nkv, int64_t edges, int32_t heads,
-                 int32_t kv_heads, int32_t D, int32_t type, const void *bias, int32_t bias_heads) {
+                 int32_t kv_heads, int32_t D, int32_t type, int64_t k_stride, int64_t v_stride,
+                 const void *bias, int32_t bias_heads) {
   if (nq < 0 || nq > 0x7fffffffll || nkv < 0 || nkv > 0x7fffffffll || edges < 0 ||
       edges > 0x7fffffffll || (edges > 0 && (nq == 0 || nkv == 0)))
     return set_error(DG_EINVAL, "%s: bad sizes", who);
@@ -733,15 +863,18 @@ int check_attend(const char *who, int64_t nq, int64_t nkv, int64_t edges, int32_
     return set_error(DG_EINVAL, "%s: heads must be a multiple of kv_heads up to %d, D 1 to %d", who,
                      DG_MAX_HEADS, DG_MAX_HEAD_DIM);
   if (!is_wide_type(type)) return set_error(DG_EINVAL, "%s: bad type", who);
+  if (k_stride > DG_MAX_STRIDE || v_stride > DG_MAX_STRIDE)
+    return set_error(DG_EINVAL, "%s: key and value rows are too far apart", who);
   if (bias && bias_heads != 1 && bias_heads != heads)
     return set_error(DG_EINVAL, "%s: bias_heads must be 1 or heads", who);
   return DG_OK;
 }
 
-// The sort of the edges by key.
+// The sort of the edges by key, for sums by groups of 2^lg lanes.
 void set_edge_sort(IdSort &so, const int32_t *indices, int64_t edges, int64_t nkv, int64_t kv_heads,
-                   int64_t D) {
+                   int64_t D, int lg) {
   memset(&so, 0, sizeof(so));
+  so.lg = lg;
   so.ids = indices;
   so.n = edges;
   so.slots = nkv;
@@ -818,8 +951,8 @@ extern "C" int dg_attend_edges(const void *q, int64_t q_stride, const void *k, i
                                const float *bias, int32_t bias_heads, float scale, void *out,
                                float *lse, int32_t *status, void *ws, size_t ws_bytes,
                                hipStream_t stream) {
-  DG_TRY(check_attend("dg_attend_edges", nq, nkv, num_edges, heads, kv_heads, D, type, bias,
-                      bias_heads));
+  DG_TRY(check_attend("dg_attend_edges", nq, nkv, num_edges, heads, kv_heads, D, type,
+                      k_stride, v_stride, bias, bias_heads));
   if (nq == 0) return DG_OK;
   const int64_t qw = (int64_t)heads * D, kw = (int64_t)kv_heads * D, b = type_bytes(type);
   if (q_stride < qw || (num_edges > 0 && (k_stride < kw || v_stride < kw)))
@@ -834,7 +967,7 @@ extern "C" int dg_attend_edges(const void *q, int64_t q_stride, const void *k, i
       ranges_overlap(out, ob, offsets, 8 * (nq + 1)) || ranges_overlap(lse, lb, bias, 4 * num_edges))
     return set_error(DG_EINVAL, "dg_attend_edges: an output overlaps an input or output");
   const size_t need = part_bytes(num_edges, (int64_t)heads * (D + 2));
-  if (num_edges > chunk_edges(num_edges) && (!ws || ws_bytes < need || ((uintptr_t)ws & 255)))
+  if (num_edges > CAP / 2 && (!ws || ws_bytes < need || ((uintptr_t)ws & 255)))
     return set_error(DG_EWORKSPACE, "dg_attend_edges: workspace needs %zu bytes", need);
   Attend a;
   memset(&a, 0, sizeof(a));
@@ -842,8 +975,8 @@ extern "C" int dg_attend_edges(const void *q, int64_t q_stride, const void *k, i
   a.k = k;
   a.v = v;
   a.q_stride = q_stride;
-  a.k_stride = k_stride;
-  a.v_stride = v_stride;
+  a.k_bytes = (uint32_t)(k_stride * b);
+  a.v_bytes = (uint32_t)(v_stride * b);
   a.offsets = offsets;
   a.indices = indices;
   a.bias = bias;
@@ -857,7 +990,7 @@ extern "C" int dg_attend_edges(const void *q, int64_t q_stride, const void *k, i
   a.D = D;
   a.scale = scale;
   a.slot = (int64_t)heads * (D + 2);
-  a.part = static_cast<float *>(ws);
+  set_parts(a, ws);
   a.status = status;
   a.out = out;
   a.lse = lse;
@@ -878,9 +1011,7 @@ extern "C" int dg_attend_edges(const void *q, int64_t q_stride, const void *k, i
       });
       return (int)DG_OK;
     });
-    if (a.chunks)
-      hipLaunchKernelGGL((k_attend_join<T, false>), dim3((unsigned)a.chunks, (unsigned)heads),
-                         dim3(JT), 0, stream, a, log2_up(D));
+    launch_join<T, false>(a, stream);
     DG_HIP(hipGetLastError());
     return (int)DG_OK;
   });
@@ -891,15 +1022,16 @@ namespace {
 // long lists, and the sort.
 struct GradRoom {
   float2 *pd;
-  int32_t *row_of;
-  float *part;
+  int32_t *row_of, *place;
+  void *part;
   size_t fixed;
 };
 GradRoom carve_grad(Carve &c, int64_t edges, int32_t heads, int32_t D) {
   GradRoom r;
   r.pd = c.take<float2>((size_t)edges * (size_t)heads);
   r.row_of = c.take<int32_t>((size_t)edges);
-  r.part = c.take<float>(part_bytes(edges, (int64_t)heads * D) / sizeof(float));
+  r.place = c.take<int32_t>((size_t)edges);
+  r.part = c.take<char>(part_bytes(edges, (int64_t)heads * D));
   r.fixed = c.used;
   return r;
 }
@@ -913,7 +1045,7 @@ extern "C" size_t dg_attend_edges_grad_workspace_bytes(int64_t num_edges, int64_
   Carve c(nullptr);
   const GradRoom r = carve_grad(c, num_edges, heads, D);
   IdSort so;
-  set_edge_sort(so, nullptr, num_edges, nkv, kv_heads, D);
+  set_edge_sort(so, nullptr, num_edges, nkv, kv_heads, D, narrowest_lg(kv_heads * D));
   return r.fixed + sort_room(so);
 }
 
@@ -924,8 +1056,8 @@ extern "C" int dg_attend_edges_grad(
     int32_t D, const int64_t *offsets, const int32_t *indices, int64_t num_edges,
     const float *bias, int32_t bias_heads, float scale, void *grad_q, void *grad_k, void *grad_v,
     float *grad_bias, int32_t *status, void *ws, size_t ws_bytes, hipStream_t stream) {
-  DG_TRY(check_attend("dg_attend_edges_grad", nq, nkv, num_edges, heads, kv_heads, D, type, bias,
-                      bias_heads));
+  DG_TRY(check_attend("dg_attend_edges_grad", nq, nkv, num_edges, heads, kv_heads, D, type,
+                      k_stride, v_stride, bias, bias_heads));
   const int64_t qw = (int64_t)heads * D, kw = (int64_t)kv_heads * D, b = type_bytes(type);
   if ((nq > 0 && (q_stride < qw || grad_stride < qw || out_stride < qw)) ||
       (nkv > 0 && (k_stride < kw || v_stride < kw)))
@@ -953,9 +1085,11 @@ extern "C" int dg_attend_edges_grad(
       if (ranges_overlap(outs[i].p, outs[i].n, outs[j].p, outs[j].n))
         return set_error(DG_EINVAL, "dg_attend_edges_grad: two outputs overlap");
   }
+  const int vph = (D + vec_of(type, D) - 1) / vec_of(type, D);  // vectors of a head
+  const RowLanes lanes = row_lanes((int64_t)kv_heads * vph);
   if (num_edges > 0) {
     IdSort so;
-    set_edge_sort(so, indices, num_edges, nkv, kv_heads, D);
+    set_edge_sort(so, indices, num_edges, nkv, kv_heads, D, lanes.lg);
     Carve size(nullptr);
     (void)carve_grad(size, num_edges, heads, D);
     carve_sort(so, size);
@@ -977,8 +1111,8 @@ extern "C" int dg_attend_edges_grad(
     a.k = k;
     a.v = v;
     a.q_stride = q_stride;
-    a.k_stride = k_stride;
-    a.v_stride = v_stride;
+    a.k_bytes = (uint32_t)(k_stride * b);
+    a.v_bytes = (uint32_t)(v_stride * b);
     a.offsets = offsets;
     a.indices = indices;
     a.bias = bias;
@@ -1003,35 +1137,36 @@ extern "C" int dg_attend_edges_grad(
     const GradRoom r = carve_grad(c, num_edges, heads, D);
     a.pd = r.pd;
     a.row_of = r.row_of;
-    a.part = r.part;
+    a.place = r.place;
+    set_parts(a, r.part);
     IdSort so;
-    set_edge_sort(so, indices, num_edges, nkv, kv_heads, D);
+    set_edge_sort(so, indices, num_edges, nkv, kv_heads, D, lanes.lg);
     carve_sort(so, c);
+    so.place = r.place;
     DG_TRY(run_sort(so, nullptr, nullptr, status, stream));
+    bool all_heads = false;
     (void)with_vec<T>(D, [&](auto v) {
       constexpr int V = decltype(v)::value;
       set_lanes(a, V);
       with_heads(a.share, [&](auto rt, auto u) {
+        all_heads = heads_in_wave(a, decltype(rt)::value);
+        a.db = grad_bias && (all_heads || bias_heads > 1) ? grad_bias : nullptr;
         hipLaunchKernelGGL((k_attend_grad_rows<T, V, decltype(rt)::value, decltype(u)::value>),
                            attend_grid(a, decltype(rt)::value), dim3(AT), 0, stream, a);
       });
-      if (a.chunks)
-        hipLaunchKernelGGL((k_attend_join<T, true>), dim3((unsigned)a.chunks, (unsigned)heads),
-                           dim3(JT), 0, stream, a, log2_up(D));
-      const int vph = (D + V - 1) / V;
-      const RowLanes lanes = row_lanes((int64_t)kv_heads * vph);
+      launch_join<T, true>(a, stream);
       const int per = AT >> lanes.lg;
       const int64_t sums = (so.chunks + per - 1) / per;
       int64_t zeros = (nkv + 8 * per - 1) / (8 * per);
       if (zeros > 4096) zeros = 4096;
       hipLaunchKernelGGL((k_attend_grad_keys<T, V>),
-                         dim3((unsigned)(sums + zeros), (unsigned)lanes.tiles), dim3(AT), 0,
-                         stream, a, so, static_cast<T *>(grad_k), static_cast<T *>(grad_v), vph,
-                         lanes.lg, sums);
+                         dim3((unsigned)(sums + zeros), (unsigned)lanes.tiles), dim3(AT),
+                         walk_bytes(so, lanes.lg), stream, a, so, static_cast<T *>(grad_k),
+                         static_cast<T *>(grad_v), vph, sums);
       return (int)DG_OK;
     });
-    if (grad_bias) {
-      const int64_t blocks = (num_edges * bias_heads + AT - 1) / AT;
+    if (grad_bias && !a.db) {
+      const int64_t blocks = (num_edges + AT - 1) / AT;
       hipLaunchKernelGGL(k_attend_grad_bias, dim3((unsigned)(blocks > 8192 ? 8192 : blocks)),
                          dim3(AT), 0, stream, a, grad_bias);
     }

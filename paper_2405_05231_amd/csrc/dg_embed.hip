@@ -14,7 +14,8 @@ namespace dg {
 namespace {
 
 constexpr int ET = 256;
-constexpr int EU = 4;  // vectors per thread (forward), rows in flight per lane (gradient)
+constexpr int EU = 4;  // vectors per thread
+constexpr int SU = 8;  // rows in flight per lane of the gradient
 
 // ------------------------------------------------------------------ forward
 // The output is one run of vectors, vpr per row, and a thread takes one of each of
@@ -101,73 +102,50 @@ int launch_rows(const void *table, int64_t N, int cols, int64_t stride, const fl
 template <typename T, typename TO, int V>
 __global__ __launch_bounds__(ET) void k_embed_sum(IdSort a, uint32_t limit, const T *src,
                                                   int64_t stride, int cols, float scale, TO *out,
-                                                  int64_t out_stride, int lg,
-                                                  int64_t sum_blocks) {
-  const int sub = threadIdx.x & ((1 << lg) - 1);
+                                                  int64_t out_stride, int64_t sum_blocks) {
+  extern __shared__ int2 s_entries[];
+  const int lg = a.lg, sub = threadIdx.x & ((1 << lg) - 1), g = threadIdx.x >> lg;
   const Piece<V> pc((blockIdx.y << lg) + sub, cols);
   const int per = ET >> lg;
   if ((int64_t)blockIdx.x >= sum_blocks) {
     const int64_t groups = ((int64_t)gridDim.x - sum_blocks) * per;
     const float zero[V] = {};
-    for (int64_t r = ((int64_t)blockIdx.x - sum_blocks) * per + (threadIdx.x >> lg); r < a.slots;
-         r += groups)
+    for (int64_t r = ((int64_t)blockIdx.x - sum_blocks) * per + g; r < a.slots; r += groups)
       if (!a.seen[r]) st_piece<false>(from_floats<TO, V>(zero), out + r * out_stride, pc);
     return;
   }
-  const int64_t c = (int64_t)blockIdx.x * per + (threadIdx.x >> lg);
+  const int64_t c = (int64_t)blockIdx.x * per + g;
   if (c >= a.chunks) return;
-  const Chunk k = chunk_of(a.dst, a.n, a.C, c);
-  const int64_t end = k.beyond ? min(k.stop + a.C, a.n) : k.stop;
-  float acc[V];
-  int32_t cur = -1;
-  bool lead = k.lead_part;
-  auto flush = [&](bool final) {
-    if ((uint32_t)cur >= limit) return;
-    const bool part = lead || (final && k.trail_part);
-    if (part) {
-      float *p = a.part + (2 * c + (lead ? 0 : 1)) * a.width;
-      Raw<float, V> r;
-      memcpy(&r.w, acc, sizeof(acc));
-      st_piece<false>(r, p, pc);
-      if (!lead && sub == 0 && blockIdx.y == 0) a.long_at[atomicAdd(a.n_long, 1)] = (int32_t)c;
-    } else {
-      float y[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) y[i] = acc[i] * scale;
-      st_piece<false>(from_floats<TO, V>(y), out + (int64_t)cur * out_stride, pc);
-    }
-    lead = false;
-  };
-  bool done = false;
-  for (int64_t i = k.begin; i < end && !done; i += EU) {
-    int32_t d[EU];
-    Raw<T, V> x[EU];
-#pragma unroll
-    for (int u = 0; u < EU; ++u) {
-      const int64_t j = min(i + u, a.n - 1);
-      d[u] = a.dst[j];
-      x[u] = ld_piece<T, V>(src + (int64_t)a.order[j] * stride, pc);
-    }
-#pragma unroll
-    for (int u = 0; u < EU; ++u) {
-      if (done || i + u >= end || (i + u >= k.stop && d[u] != k.last)) {
-        done = true;
-        continue;
-      }
-      float y[V];
-      to_floats<T, V>(x[u], y);
-      if (i + u == k.begin || d[u] != cur) {
-        if (i + u != k.begin) flush(false);
-        cur = d[u];
-#pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] = y[e];
-      } else {
+  src += pc.at;
+  float acc[V] = {};
+  Raw<T, V> x[SU];
+  walk_chunk<SU>(
+      a, a.order, limit, 1, lg, c, s_entries + g * a.C,
+      [&](int u, int64_t, int32_t place, int, bool ok) {
+        x[u] = ld_raw<T, V>(src + (int64_t)place * stride);
+        if (!ok) x[u].w = typename Raw<T, V>::W(0);
+      },
+      [&](int u) {
+        float y[V];
+        to_floats<T, V>(x[u], y);
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[e] += y[e];
-      }
-    }
-  }
-  if (k.begin < end) flush(true);
+      },
+      [&](int32_t node, int part) {
+        if ((uint32_t)node < limit && part < 2) {
+          Raw<float, V> r;
+          memcpy(&r.w, acc, sizeof(acc));
+          st_piece<false>(r, a.part + (2 * c + part) * a.width, pc);
+          if (part && sub == 0 && blockIdx.y == 0)
+            a.long_at[atomicAdd(a.n_long, 1)] = LongAt{(int32_t)c, node};
+        } else if ((uint32_t)node < limit) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) acc[e] *= scale;
+          st_piece<true>(from_floats<TO, V>(acc), out + (int64_t)node * out_stride, pc);
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = 0.f;
+      });
 }
 
 // A block per long segment: its groups of lanes add every NG-th partial sum, then one
@@ -178,12 +156,22 @@ __global__ __launch_bounds__(ET) void k_join(IdSort a, JoinOut o, int cols, int 
   const int z = blockIdx.z;
   const int sub = threadIdx.x & ((1 << lg) - 1), g = threadIdx.x >> lg, groups = ET >> lg;
   const Piece<V> pc((blockIdx.y << lg) + sub, cols);
+  // (the grid is within the list's room)
+  LongAt first = a.long_at[blockIdx.x];
   const int many = *a.n_long;
   for (int l = blockIdx.x; l < many; l += gridDim.x) {
-    const int64_t c = a.long_at[l];
-    const int32_t node = a.dst[(c + 1) * a.C - 1];
-    // last chunk that starts with the node: chunk c + 1 does
+    const LongAt at_l = l == (int)blockIdx.x ? first : a.long_at[l];
+    const int64_t c = at_l.chunk;
+    const int32_t node = at_l.node;
+    // last chunk that starts with the node: chunk c + 1 does; most are within the reach
+    // of the block's threads
     int64_t lo = c + 1, hi = a.chunks;
+    {
+      const int64_t at = lo + threadIdx.x;
+      const int ok = __syncthreads_count(at < hi && a.dst[min(at, hi - 1) * a.C] == node);
+      if (ok < ET) hi = lo + ok;
+      lo += ok - 1;
+    }
     while (hi - lo > 1) {
       const int64_t step = (hi - lo + ET - 1) / ET;
       const int64_t at = lo + (int64_t)threadIdx.x * step;
@@ -235,8 +223,11 @@ int64_t zero_blocks(const IdSort &a, int lg) {
   return b > 4096 ? 4096 : b;
 }
 
-void set_sort(IdSort &a, const int32_t *ids, int64_t n, int64_t N, int64_t D, bool compact) {
+// The sort of a list for sums of rows of D elements by groups of 2^lg lanes.
+void set_sort(IdSort &a, const int32_t *ids, int64_t n, int64_t N, int64_t D, bool compact,
+              int lg) {
   memset(&a, 0, sizeof(a));
+  a.lg = lg;
   a.ids = ids;
   a.n = n;
   a.slots = N;
@@ -305,7 +296,7 @@ extern "C" size_t dg_embed_rows_grad_workspace_bytes(int64_t N, int64_t D, int64
                                                      int32_t sparse) {
   if (n < 0 || n > 0x7fffffffll || N < 1 || N > 0x7fffffffll || D < 1 || D > DG_MAX_COLS) return 0;
   IdSort a;
-  set_sort(a, nullptr, n, N, D, sparse != 0);
+  set_sort(a, nullptr, n, N, D, sparse != 0, narrowest_lg(D));
   return sort_room(a);
 }
 
@@ -331,7 +322,8 @@ extern "C" int dg_embed_rows_grad(const void *grad_out, int32_t type, int64_t gr
       ranges_overlap(grad, out_bytes, ids, 4 * n) || ranges_overlap(rows, 4 * out_rows, ids, 4 * n))
     return set_error(DG_EINVAL, "dg_embed_rows_grad: an output overlaps an input");
   IdSort a;
-  set_sort(a, ids, n, N, D, sparse);
+  const RowLanes lanes = row_lanes((D + vec_of(type, D) - 1) / vec_of(type, D));
+  set_sort(a, ids, n, N, D, sparse, lanes.lg);
   Carve size(nullptr);
   carve_sort(a, size);
   if (!ws || ws_bytes < size.used || ((uintptr_t)ws & 255))
@@ -346,13 +338,12 @@ extern "C" int dg_embed_rows_grad(const void *grad_out, int32_t type, int64_t gr
       using TO = decltype(o);
       return with_vec<T>(D, [&](auto v) {
         constexpr int V = decltype(v)::value;
-        const RowLanes r = row_lanes((D + V - 1) / V);
-        const int per = ET >> r.lg;
+        const int per = ET >> a.lg;
         const int64_t sums = (a.chunks + per - 1) / per;
         hipLaunchKernelGGL((k_embed_sum<T, TO, V>),
-                           dim3((unsigned)(sums + zero_blocks(a, r.lg)), (unsigned)r.tiles),
-                           dim3(ET), 0, stream, a, a.limit(), (const T *)grad_out, grad_stride,
-                           (int)D, scale, (TO *)grad, D, r.lg, sums);
+                           dim3((unsigned)(sums + zero_blocks(a, a.lg)), (unsigned)lanes.tiles),
+                           dim3(ET), walk_bytes(a, a.lg), stream, a, a.limit(),
+                           (const T *)grad_out, grad_stride, (int)D, scale, (TO *)grad, D, sums);
         DG_HIP(hipGetLastError());
         const JoinOut j = {{grad, nullptr}, {D, 0}, {0, 0}, {scale, 0.f}};
         return run_join(a, j, 1, (int)D, grad_type, stream);

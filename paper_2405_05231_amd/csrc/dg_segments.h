@@ -15,22 +15,27 @@
 
 namespace dg {
 
+struct LongAt {
+  int32_t chunk, node;
+};
 // A list of n IDs in [0, slots) and its stable sort.  An ID of -1 stands for no
 // node; it and IDs outside [0, slots) sort behind all others as `slots`.
 struct IdSort {
   const int32_t *ids;
   int64_t n, slots;
   bool compact;        // dst = rank among the distinct nodes, not the node
+  int lg;              // lanes that take a chunk: 2^lg
   // carved
   int32_t *key[2], *pos[2];  // keys and list places, alternating between passes
   int32_t *dst;        // [n] row that each sorted entry is added to: below limit(), or
                        // the entry is of no node (those are the last)
-  int32_t *order;      // [n] list place of each sorted entry
+  int32_t *order;      // [n] list place of each sorted entry, or (with place) unset
+  int32_t *place;      // set by the caller, or NULL: [n] where each list entry is sorted to
   uint8_t *seen;       // [slots] whether the node occurs (!compact)
   uint32_t *cnt, *tot; // digit counts per tile, and in all
   int32_t *heads;      // distinct nodes per block of entries, then before it (compact)
   int32_t *n_long;     // long segments listed
-  int32_t *long_at;    // [n / C + 1] the chunk in which each starts
+  LongAt *long_at;     // [n / C + 1] the chunk in which each starts, and its node
   float *part;         // [2 * chunks][width] partial sums
   int32_t C;           // entries of a chunk
   int64_t chunks;
@@ -46,43 +51,91 @@ size_t sort_room(IdSort a);
 // (compact).  status: ORs 1 where an ID is below -1 or not below slots (optional).
 int run_sort(IdSort &a, int32_t *node_out, int64_t *count, int32_t *status, hipStream_t s);
 
-// What the group of lanes that takes chunk c does: entries [begin, stop) in order;
-// a segment ends where dst changes.
-struct Chunk {
-  int64_t begin, stop;   // stop: the chunk's end
-  int32_t last;          // dst of its last entry
-  bool lead_part;        // entries from `begin` that continue a long segment
-  bool trail_part;       // the last segment is long and starts here
-  bool beyond;           // the last segment goes on past `stop`, into the next chunk only
-};
-__device__ __forceinline__ Chunk chunk_of(const int32_t *dst, int64_t n, int C, int64_t c) {
-  Chunk k;
-  const int64_t lo = c * C, hi = min(lo + C, n);
-  // the places that decide, loaded together
-  const int32_t first = dst[lo], last = dst[hi - 1];
-  const int32_t before = dst[max(lo - 1, (int64_t)0)];
-  const int32_t before2 = dst[max(lo - C - 1, (int64_t)0)];
-  const int32_t after = dst[min(hi, n - 1)];
-  const int32_t after2 = dst[min(hi + C, n - 1)];
-  const bool lead = lo > 0 && before == first;
-  k.begin = lo;
-  k.stop = hi;
-  k.last = last;
-  // it starts two chunks back, or in the last one and reaches the next
-  k.lead_part = lead && ((lo > C && before2 == first) || (hi < n && after == first));
-  if (lead && !k.lead_part) {  // the chunk before adds these
-    int64_t a = lo, b = hi;    // first entry of another segment, in (a, b]
-    while (b - a > 1) {
-      const int64_t m = (a + b) >> 1;
-      if (dst[m] == first) a = m; else b = m;
+// The work of the group of 2^lg lanes that takes chunk c.  `mine` (C entries of shared
+// memory, the group's own) first receives the chunk's entries, so that one wait brings the
+// places of all rows that the chunk adds, and rows are waited for U at a time:
+//   load(u, i, x, t, ok)  step u reads row x = other[i] of sorted entry i (t-th of `share`
+//                         steps of it); !ok: what it adds has to be 0
+//   add(u)                adds it
+//   flush(node, part)     ends the segment of `node`: part 0 or 1 is a partial sum of a
+//                         long segment (that goes on from the chunk before, or starts
+//                         here), 2 the whole sum; the next segment starts from 0
+template <int U, typename Load, typename Add, typename Flush>
+__device__ __forceinline__ void walk_chunk(const IdSort &a, const int32_t *other, uint32_t limit,
+                                           int share, int lg, int64_t c, int2 *mine, Load load,
+                                           Add add, Flush flush) {
+  const int sub = threadIdx.x & ((1 << lg) - 1);
+  const int64_t n = a.n, lo = c * a.C, hi = min(lo + a.C, n);
+  const int32_t before = a.dst[max(lo - 1, (int64_t)0)];
+  const int32_t before2 = a.dst[max(lo - a.C - 1, (int64_t)0)];
+  const int32_t after = a.dst[min(hi, n - 1)];
+  const int32_t after2 = a.dst[min(hi + a.C, n - 1)];
+  auto fetch = [&](int64_t from) {
+    for (int i = sub; i < a.C; i += 1 << lg) {
+      const int64_t j = min(from + i, n - 1);
+      mine[i] = int2{a.dst[j], other[j]};
     }
-    k.begin = b;
+    __builtin_amdgcn_wave_barrier();  // (a group is within a wave, whose LDS runs in order)
+  };
+  fetch(lo);
+  const int many = (int)(hi - lo);
+  const int32_t first = mine[0].x, last = mine[many - 1].x;
+  // the first segment comes from the chunk before: long if it starts two chunks back, or
+  // in the last one and reaches the next; else the group of the chunk before adds it
+  const bool from_before = lo > 0 && before == first;
+  bool lead = from_before && ((lo > a.C && before2 == first) || (hi < n && after == first));
+  int begin = 0;
+  if (from_before && !lead) {
+    int x = 0, y = many;  // first entry of another segment, in (x, y]
+    while (y - x > 1) {
+      const int m = (x + y) >> 1;
+      if (mine[m].x == first) x = m; else y = m;
+    }
+    begin = y;
   }
-  const bool starts = !(lead && last == first);  // the last segment starts here
-  const bool on = starts && hi < n && after == last;
-  k.trail_part = on && hi + C < n && after2 == last;
-  k.beyond = on && !k.trail_part;
-  return k;
+  if (begin == many) return;
+  // the last segment goes on: into the next chunk only, or it is long
+  const bool on = !(from_before && last == first) && hi < n && after == last;
+  const bool trail = on && hi + a.C < n && after2 == last;
+  int32_t cur = mine[begin].x;
+#pragma unroll 1
+  for (int pass = 0;; ++pass) {
+    const int64_t base = pass ? hi : lo;
+    const int end = pass ? (int)min((int64_t)a.C, n - hi) : many;
+    if (pass) fetch(hi);
+    int e = pass ? 0 : begin, t = 0;
+    while (e < end) {
+      int32_t d[U];
+      bool in[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int j = min(e, end - 1);
+        const int2 x = mine[j];
+        d[u] = x.x;
+        in[u] = e < end && (!pass || x.x == last);
+        load(u, base + j, x.y, t, in[u] && (uint32_t)x.x < limit);
+        const bool next = ++t >= share;
+        e += next;
+        t = next ? 0 : t;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (in[u] && d[u] != cur) {
+          flush(cur, lead ? 0 : 2);
+          lead = false;
+          cur = d[u];
+        }
+        add(u);
+      }
+      if (!in[U - 1]) break;
+    }
+    if (pass || !on || trail) break;
+  }
+  flush(cur, lead ? 0 : trail ? 1 : 2);
+}
+// Shared memory of a block of 256 threads for it.
+inline size_t walk_bytes(const IdSort &a, int lg) {
+  return (size_t)(256 >> lg) * (size_t)a.C * sizeof(int2);
 }
 
 // Joins the partial sums of the long segments: output z (of up to two) takes columns
@@ -106,5 +159,13 @@ inline RowLanes row_lanes(int64_t vecs) {
   const int64_t t64 = (vecs + 63) / 64, t32 = (vecs + 31) / 32;
   return t32 * 32 < t64 * 64 ? RowLanes{5, (int)t32} : RowLanes{6, (int)t64};
 }
+
+// Elements per vector of rows of `cols` elements, as with_vec chooses them.
+inline int vec_of(int32_t type, int64_t cols) {
+  const int v = 16 / type_bytes(type);
+  return cols >= v ? v : 1;
+}
+// The fewest lanes that a chunk can get at this width, whatever the type.
+inline int narrowest_lg(int64_t width) { return width > 16 ? 2 : 0; }
 
 }  // namespace dg

@@ -20,7 +20,8 @@ constexpr int HEADS = 1024;        // entries of a block of k_heads_*
 
 // Rounds of 64 entries that a wave takes of its tile: short tiles until they fill
 // the chip.
-int sort_rounds(int64_t n) { return n > (1 << 20) ? 16 : 4; }
+constexpr int BIG_ROUNDS = 8;
+int sort_rounds(int64_t n) { return n > (1 << 20) ? BIG_ROUNDS : 4; }
 
 __device__ __forceinline__ int32_t sort_key(int32_t id, int64_t slots, bool *bad) {
   const bool ok = id >= 0 && (int64_t)id < slots;
@@ -42,6 +43,7 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, uint64_t ac
 struct Pass {
   const int32_t *key, *pos;  // pos NULL: the list itself (key = ids)
   int32_t *key_out, *pos_out;
+  int32_t *place;  // the last pass: where each list entry goes, instead of pos_out
   int shift, bits;
   int64_t tiles;
 };
@@ -107,7 +109,9 @@ __global__ __launch_bounds__(ST) void k_sort_place(IdSort a, Pass p) {
   const int bins = 1 << p.bits;
   for (int i = threadIdx.x; i < SW * BINS; i += ST) (&s_at[0][0])[i] = 0;
   __syncthreads();
-  const int64_t t0 = (int64_t)blockIdx.x * (ST * R) + w * (64 * R);
+  // neighbouring tiles, whose entries of a digit lie side by side, meet in one L2
+  const int64_t tile = xcd_block(blockIdx.x, gridDim.x);
+  const int64_t t0 = tile * (ST * R) + w * (64 * R);
   int32_t k[R], v[R];
   uint32_t rank[R];
 #pragma unroll
@@ -149,7 +153,7 @@ __global__ __launch_bounds__(ST) void k_sort_place(IdSort a, Pass p) {
   for (int q = 0; q < PER; ++q) {
     const int d = threadIdx.x * PER + q;
     if (d < bins) {
-      uint32_t next = (uint32_t)first + a.cnt[(int64_t)d * p.tiles + blockIdx.x];
+      uint32_t next = (uint32_t)first + a.cnt[(int64_t)d * p.tiles + tile];
 #pragma unroll
       for (int j = 0; j < SW; ++j) {
         const uint32_t own = s_at[j][d];
@@ -166,7 +170,8 @@ __global__ __launch_bounds__(ST) void k_sort_place(IdSort a, Pass p) {
     const uint32_t d = ((uint32_t)k[r] >> p.shift) & (bins - 1);
     const uint32_t to = at[d] + rank[r];
     p.key_out[to] = k[r];
-    p.pos_out[to] = v[r];
+    if (p.place) p.place[v[r]] = (int32_t)to;
+    else p.pos_out[to] = v[r];
   }
 }
 
@@ -276,7 +281,8 @@ __global__ __launch_bounds__(SMALL_T) void k_sort_small(IdSort a, int32_t *node_
     if (i >= n) break;
     const int32_t k = (int32_t)(s[i] >> 32);
     at += head[r];
-    a.order[i] = (int32_t)(uint32_t)s[i];
+    if (a.place) a.place[(uint32_t)s[i]] = i;
+    else a.order[i] = (int32_t)(uint32_t)s[i];
     a.dst[i] = !a.compact ? k : k < a.slots ? (int32_t)at : -1;
     if (a.compact && head[r]) node_out[at] = k;
   }
@@ -284,12 +290,16 @@ __global__ __launch_bounds__(SMALL_T) void k_sort_small(IdSort a, int32_t *node_
 
 }  // namespace
 
-// Entries of a chunk: shorter ones until their groups of lanes fill the chip.
-static int chunk_len(int64_t n) { return n >= (1 << 20) ? 64 : n >= (1 << 17) ? 32 : 16; }
+// Entries of a chunk: shorter ones until their groups of lanes fill the chip, and where
+// groups are so narrow that a block would need over 32 KB for its chunks.
+static int chunk_len(int64_t n, int lg) {
+  const int c = n >= (1 << 20) ? 64 : n >= (1 << 17) ? 32 : 16;
+  return lg < 2 && c > 16 << lg ? 16 << lg : c;
+}
 
 void carve_sort(IdSort &a, Carve &c) {
   const int64_t n = a.n;
-  a.C = chunk_len(n);
+  a.C = chunk_len(n, a.lg);
   a.chunks = (n + a.C - 1) / a.C;
   const int64_t tiles = (n + ST * sort_rounds(n) - 1) / (ST * sort_rounds(n));
   for (int i = 0; i < 2; ++i) {
@@ -304,7 +314,7 @@ void carve_sort(IdSort &a, Carve &c) {
   a.tot = c.take<uint32_t>(BINS);
   a.heads = a.compact ? c.take<int32_t>((size_t)((n + HEADS - 1) / HEADS)) : nullptr;
   a.n_long = c.take<int32_t>(1);
-  a.long_at = c.take<int32_t>((size_t)a.chunks + 1);
+  a.long_at = c.take<LongAt>((size_t)a.chunks + 1);
   a.part = n > 2 * a.C ? c.take<float>((size_t)(2 * a.chunks * a.width)) : nullptr;
 }
 
@@ -344,6 +354,7 @@ int run_sort(IdSort &a, int32_t *node_out, int64_t *count, int32_t *status, hipS
     p.pos = i ? a.pos[in] : nullptr;
     p.key_out = a.key[out];
     p.pos_out = a.pos[out];
+    p.place = i == passes - 1 ? a.place : nullptr;
     p.shift = i * each;
     p.bits = total - p.shift < each ? total - p.shift : each;
     const dim3 g((unsigned)p.tiles), b(ST);
@@ -356,9 +367,9 @@ int run_sort(IdSort &a, int32_t *node_out, int64_t *count, int32_t *status, hipS
       hipLaunchKernelGGL((k_sort_place<R, F>), g, b, 0, s, a, p);
     };
     using std::integral_constant;
-    if (rounds == 16) {
-      if (i == 0) go(integral_constant<int, 16>(), std::true_type());
-      else go(integral_constant<int, 16>(), std::false_type());
+    if (rounds == BIG_ROUNDS) {
+      if (i == 0) go(integral_constant<int, BIG_ROUNDS>(), std::true_type());
+      else go(integral_constant<int, BIG_ROUNDS>(), std::false_type());
     } else {
       if (i == 0) go(integral_constant<int, 4>(), std::true_type());
       else go(integral_constant<int, 4>(), std::false_type());
