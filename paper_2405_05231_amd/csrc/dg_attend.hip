@@ -61,8 +61,8 @@ struct Attend {
   int64_t go_stride, o_stride;
   const float *lse_in;
   const int32_t *place;  // [edges] place of each edge in the order of the keys
-  float2 *pd;            // [edges][heads] p and ds, in that order
-  int32_t *row_of;       // [edges] row, in that order
+  float2 *pd;            // [edges + 1][heads] p and ds, in that order
+  int32_t *row_of;       // [edges + 1] row, in that order
   void *dq;
   float *db;             // [edges][bias_heads] or NULL
 };
@@ -84,8 +84,10 @@ __device__ __forceinline__ float dot(const Raw<T, V> &x, const Raw<T, V> &y) {
 }
 
 // What a lane is for.
-template <typename T, int V, int RT>
+// LG: log2 of the lanes of a head where the compiler knows it, or -1.
+template <typename T, int V, int RT, int LG>
 struct Lane {
+  static __device__ __forceinline__ int lg_g(const Attend &a) { return LG >= 0 ? LG : a.lg_g; }
   Piece<V> pc;
   int es, rs;       // edge and row within the wave
   int kvh, h0;      // key head, first query head
@@ -95,18 +97,18 @@ struct Lane {
   const char *k, *v;  // its vector of row 0 of the keys and values
   typename Raw<T, V>::W mask;  // ones where the element is this lane's own
   __device__ __forceinline__ Lane(const Attend &a, int lg_e)
-      : pc((int)(threadIdx.x & ((1 << a.lg_g) - 1)), a.D) {
+      : pc((int)(threadIdx.x & ((1 << lg_g(a)) - 1)), a.D) {
     const int lane = threadIdx.x & 63;
     const int parts = a.share / RT;
     const int tile = blockIdx.y / parts;
-    const int h = (tile << a.lg_h) + ((lane >> a.lg_g) & ((1 << a.lg_h) - 1));
-    es = (lane >> (a.lg_g + a.lg_h)) & ((1 << lg_e) - 1);
-    rs = lane >> (a.lg_g + a.lg_h + lg_e);
+    const int h = (tile << a.lg_h) + ((lane >> lg_g(a)) & ((1 << a.lg_h) - 1));
+    es = (lane >> (lg_g(a) + a.lg_h)) & ((1 << lg_e) - 1);
+    rs = lane >> (lg_g(a) + a.lg_h + lg_e);
     head = h < a.kv_heads;
     kvh = min(h, a.kv_heads - 1);
     h0 = kvh * a.share + (blockIdx.y - tile * parts) * RT;
-    first = (lane & ((1 << a.lg_g) - 1)) == 0;
-    ragged = (V << a.lg_g) != a.D;
+    first = (lane & ((1 << lg_g(a)) - 1)) == 0;
+    ragged = (V << lg_g(a)) != a.D;
     k = (const char *)(static_cast<const T *>(a.k) + kvh * a.D + pc.at);
     v = (const char *)(static_cast<const T *>(a.v) + kvh * a.D + pc.at);
     typedef std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t> Word;
@@ -120,12 +122,20 @@ struct Lane {
     if (ragged) x.w &= mask;
     return x;
   }
+  // h0, for the addresses of one row: hidden from the compiler, which would keep those of
+  // every head in registers from row to row
+  __device__ __forceinline__ int head0() const {
+    int h = h0;
+    asm("" : "+v"(h));
+    return h;
+  }
   // A row's vectors of the RT heads from h0; elements of other lanes are 0.
   __device__ __forceinline__ void heads_of(const void *p, int64_t row, int64_t stride, int D,
                                            Raw<T, V> (&x)[RT]) const {
+    const T *at = static_cast<const T *>(p) + row * stride + (head0() * D + pc.at);
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      x[t] = ld_piece<T, V>(static_cast<const T *>(p) + row * stride + (h0 + t) * D, pc);
+      x[t] = ld_raw<T, V>(at + t * D);
       x[t].w &= mask;
     }
   }
@@ -198,8 +208,17 @@ __device__ __forceinline__ Staged stage(const Attend &a, Stage *s, int64_t e0, i
   return g;
 }
 
+// Steps of U edges per edge slot that the longest of the wave's lists takes (the same
+// number for the whole wave, in a scalar register).
+template <int U>
+__device__ __forceinline__ int steps_of(int lanes_lg, int start, int end, int lg_e) {
+  uint32_t n[1] = {(uint32_t)(end - start)};
+  lanes_reduce<false>(n, lanes_lg + lg_e, 6, MaxU());
+  return (__builtin_amdgcn_readfirstlane((int)n[0]) + (U << lg_e) - 1) / U >> lg_e;
+}
+
 // The part of a list that one wave reads at a time: U edges of each edge slot.
-template <typename T, int V, int RT, int U>
+template <typename T, int V, int RT, int U, int LG>
 struct Edges {
   Raw<T, V> k[U], v[U];
   float b[U][RT];
@@ -208,7 +227,7 @@ struct Edges {
   int e[U];
   // base: the same in a row slot; edges from `end` on are none.
   template <bool GRAD>
-  __device__ __forceinline__ void load(const Attend &a, const Lane<T, V, RT> &ln, const Staged &g,
+  __device__ __forceinline__ void load(const Attend &a, const Lane<T, V, RT, LG> &ln, const Staged &g,
                                        int base, int end, int lg_e, bool *bad) {
     int32_t j[U];
 #pragma unroll
@@ -265,29 +284,31 @@ struct Edges {
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int t = 0; t < RT; ++t) asm("" : "+v"(b[u][t]));
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int t = 0; t < RT; ++t) b[u][t] = 0.f;
     }
   }
   // Scores: -inf for no edge and for a masked one, whatever its key holds.
-  __device__ __forceinline__ void scores(const Attend &a, const Lane<T, V, RT> &ln,
+  __device__ __forceinline__ void scores(const Attend &a, const Lane<T, V, RT, LG> &ln,
                                          const Raw<T, V> (&q)[RT], float (&s)[U * RT]) const {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const Raw<T, V> x = ln.own(k[u]);
 #pragma unroll
       for (int t = 0; t < RT; ++t) s[u * RT + t] = dot<T, V>(q[t], x);
+      if (RT > 1) __builtin_amdgcn_sched_barrier(0);
     }
-    group_sum(s, a.lg_g);
+    group_sum(s, Lane<T, V, RT, LG>::lg_g(a));
+    if (a.bias) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        s[u * RT + t] = ok[u] && b[u][t] != NINF ? s[u * RT + t] * a.scale + b[u][t] : NINF;
-      }
+        for (int t = 0; t < RT; ++t)
+          s[u * RT + t] = ok[u] && b[u][t] != NINF ? s[u * RT + t] * a.scale + b[u][t] : NINF;
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) s[u * RT + t] = ok[u] ? s[u * RT + t] * a.scale : NINF;
+    }
   }
 };
 
@@ -322,8 +343,8 @@ struct State {
 
 // Attends over edges [start, end) of this lane's row, all lanes of the wave together;
 // every lane of the row has the whole result.
-template <typename T, int V, int RT, int U>
-__device__ __forceinline__ void attend_list(const Attend &a, const Lane<T, V, RT> &ln,
+template <typename T, int V, int RT, int U, int LG>
+__device__ __forceinline__ void attend_list(const Attend &a, const Lane<T, V, RT, LG> &ln,
                                             const Raw<T, V> (&q)[RT], const Staged &g, int start,
                                             int end, int lg_e, State<T, V, RT> &st, bool *bad) {
 #pragma unroll
@@ -333,22 +354,39 @@ __device__ __forceinline__ void attend_list(const Attend &a, const Lane<T, V, RT
 #pragma unroll
     for (int i = 0; i < V; ++i) st.acc[t][i] = 0.f;
   }
-  for (int base = start; __ballot(base < end) != 0; base += U << lg_e) {
-    Edges<T, V, RT, U> ed;
+  const int steps = steps_of<U>(Lane<T, V, RT, LG>::lg_g(a) + a.lg_h, start, end, lg_e);
+  int base = start;
+#pragma unroll 1
+  for (int i = 0; i < steps; ++i, base += U << lg_e) {
+    Edges<T, V, RT, U, LG> ed;
     ed.template load<false>(a, ln, g, base, end, lg_e, bad);
     float s[U * RT];
     ed.scores(a, ln, q, s);
+    // m need not be the largest score, only near it: it moves (and the sums with it) where a
+    // score is above it by more than 8, which exp and the 32-bit sums take with ease
+    float top[RT];
+    bool move = false;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      float top = st.m[t];
+      top[t] = s[t];
 #pragma unroll
-      for (int u = 0; u < U; ++u) top = fmaxf(top, s[u * RT + t]);
-      const float from = top == NINF ? 0.f : top;  // no edge yet
-      const float f = exp_of(st.m[t] - from);
-      st.m[t] = top;
-      st.l[t] *= f;
+      for (int u = 1; u < U; ++u) top[t] = fmaxf(top[t], s[u * RT + t]);
+      move |= top[t] > st.m[t] + 8.f;
+    }
+    if (__ballot(move) != 0) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) st.acc[t][i] *= f;
+      for (int t = 0; t < RT; ++t) {
+        const float m = fmaxf(top[t], st.m[t]);
+        const float f = m == NINF ? 1.f : exp_of(st.m[t] - m);
+        st.m[t] = m;
+        st.l[t] *= f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) st.acc[t][i] *= f;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const float from = st.m[t] == NINF ? 0.f : st.m[t];  // no edge yet
 #pragma unroll
       for (int u = 0; u < U; ++u) s[u * RT + t] = exp_of(s[u * RT + t] - from);
     }
@@ -363,10 +401,11 @@ __device__ __forceinline__ void attend_list(const Attend &a, const Lane<T, V, RT
         st.l[t] += p[t];
       }
       add_weighted<T, V, RT>(ed.v[u], p, some, a.bias_heads > 1, st.acc);
+      if (RT > 1) __builtin_amdgcn_sched_barrier(0);
     }
   }
   // the edge slots of a row
-  const int from = a.lg_g + a.lg_h, to = from + lg_e;
+  const int from = Lane<T, V, RT, LG>::lg_g(a) + a.lg_h, to = from + lg_e;
   if (from == to) return;
   float top[RT];
 #pragma unroll
@@ -380,6 +419,7 @@ __device__ __forceinline__ void attend_list(const Attend &a, const Lane<T, V, RT
 #pragma unroll
     for (int i = 0; i < V; ++i) st.acc[t][i] *= f;
     lanes_reduce<false>(st.acc[t], from, to, AddF());
+    if (RT > 1) __builtin_amdgcn_sched_barrier(0);  // (a head at a time: fewer registers)
   }
   lanes_reduce<false>(st.l, from, to, AddF());
 }
@@ -394,8 +434,8 @@ __device__ __forceinline__ void take_work(const Attend &a, Stage *s, Task task) 
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int lane = threadIdx.x & 63;
   const bool by_rows = (int64_t)blockIdx.x >= a.chunk_blocks;
-  const int lg_e = by_rows ? a.lg_e : 6 - a.lg_g - a.lg_h;
-  const int slots = 64 >> (a.lg_g + a.lg_h + lg_e);  // 1 for chunks
+  const int lg_e = by_rows ? a.lg_e : 6 - LaneT::lg_g(a) - a.lg_h;
+  const int slots = 64 >> (LaneT::lg_g(a) + a.lg_h + lg_e);  // 1 for chunks
   const int64_t unit =
       ((int64_t)blockIdx.x - (by_rows ? a.chunk_blocks : 0)) * AW + wave;  // wave or chunk
   int64_t r0 = 0, off, first = -1, last = -1;
@@ -457,10 +497,10 @@ __device__ __forceinline__ void take_work(const Attend &a, Stage *s, Task task) 
   }
 }
 
-template <typename T, int V, int RT, int U>
-__global__ __launch_bounds__(AT, RT == 4 ? 2 : RT == 2 ? 3 : 4) void k_attend(Attend a) {
+template <typename T, int V, int RT, int U, int LG>
+__global__ __launch_bounds__(AT, RT == 1 ? 5 : 3) void k_attend(Attend a) {
   __shared__ Stage s_stage[AW];
-  typedef Lane<T, V, RT> L;
+  typedef Lane<T, V, RT, LG> L;
   bool bad = false;
   take_work<false, L>(
       a, &s_stage[__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))],
@@ -468,12 +508,13 @@ __global__ __launch_bounds__(AT, RT == 4 ? 2 : RT == 2 ? 3 : 4) void k_attend(At
         Raw<T, V> q[RT];
         State<T, V, RT> st;
         ln.heads_of(a.q, row, a.q_stride, a.D, q);
-        attend_list<T, V, RT, U>(a, ln, q, g, start, end, lg_e, st, &bad);
+        attend_list<T, V, RT, U, LG>(a, ln, q, g, start, end, lg_e, st, &bad);
         if (slot == -2 || !ln.head || ln.es) return;
         float *part = a.part + slot * a.slot;
+        const int h0 = ln.head0();
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-          const int h = ln.h0 + t;
+          const int h = h0 + t;
           if (slot >= 0) {
             Raw<float, V> r;
             memcpy(&r.w, st.acc[t], sizeof(st.acc[t]));
@@ -583,8 +624,8 @@ __global__ __launch_bounds__(JT) void k_attend_join(Attend a, int lg) {
 }
 
 // ------------------------------------------------------------------ gradient by rows
-template <typename T, int V, int RT, int U>
-__device__ __forceinline__ void grad_list(const Attend &a, const Lane<T, V, RT> &ln, int64_t row,
+template <typename T, int V, int RT, int U, int LG>
+__device__ __forceinline__ void grad_list(const Attend &a, const Lane<T, V, RT, LG> &ln, int64_t row,
                                           const Staged &g, int start, int end, int lg_e,
                                           float (&dq)[RT][V], bool *bad) {
   Raw<T, V> q[RT], go[RT];
@@ -594,19 +635,25 @@ __device__ __forceinline__ void grad_list(const Attend &a, const Lane<T, V, RT> 
   {
     Raw<T, V> o[RT];
     ln.heads_of(a.o, row, a.o_stride, a.D, o);
+    const int h0 = ln.head0();
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       delta[t] = dot<T, V>(go[t], o[t]);
-      lse[t] = a.lse_in[row * a.heads + ln.h0 + t];
+      // a row without weight (lse = -inf) has no gradient: exp(s - inf) is 0
+      lse[t] = a.lse_in[row * a.heads + h0 + t];
+      lse[t] = lse[t] == NINF ? -NINF : lse[t];
     }
   }
-  group_sum(delta, a.lg_g);
+  group_sum(delta, Lane<T, V, RT, LG>::lg_g(a));
 #pragma unroll
   for (int t = 0; t < RT; ++t)
 #pragma unroll
     for (int i = 0; i < V; ++i) dq[t][i] = 0.f;
-  for (int base = start; __ballot(base < end) != 0; base += U << lg_e) {
-    Edges<T, V, RT, U> ed;
+  const int steps = steps_of<U>(Lane<T, V, RT, LG>::lg_g(a) + a.lg_h, start, end, lg_e);
+  int base = start;
+#pragma unroll 1
+  for (int i = 0; i < steps; ++i, base += U << lg_e) {
+    Edges<T, V, RT, U, LG> ed;
     ed.template load<true>(a, ln, g, base, end, lg_e, bad);
     float s[U * RT], dp[U * RT];
     ed.scores(a, ln, q, s);
@@ -616,64 +663,74 @@ __device__ __forceinline__ void grad_list(const Attend &a, const Lane<T, V, RT> 
 #pragma unroll
       for (int t = 0; t < RT; ++t) dp[u * RT + t] = dot<T, V>(go[t], x);
     }
-    group_sum(dp, a.lg_g);
+    group_sum(dp, Lane<T, V, RT, LG>::lg_g(a));
     float sum[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float ds[RT];
+      float ds[RT], p[RT];
       bool some[RT];
       sum[u] = 0.f;
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        // a row without weight has lse = -inf and no gradient
-        const float p = lse[t] == NINF ? 0.f : exp_of(s[u * RT + t] - lse[t]);
-        some[t] = p != 0.f;
-        ds[t] = some[t] ? p * (dp[u * RT + t] - delta[t]) : 0.f;
+        p[t] = exp_of(s[u * RT + t] - lse[t]);
+        some[t] = p[t] != 0.f;
+        ds[t] = some[t] ? p[t] * (dp[u * RT + t] - delta[t]) : 0.f;
         sum[u] += ds[t];
-        if (ln.first && ln.head && ed.in[u]) a.pd[(int64_t)ed.to[u] * a.heads + ln.h0 + t] = float2{p, ds[t]};
-        if (a.db && a.bias_heads > 1 && ln.first && ln.head && ed.in[u])
-          a.db[(g.e0 + ed.e[u]) * a.bias_heads + ln.h0 + t] = ds[t];
       }
       add_weighted<T, V, RT>(ed.k[u], ds, some, a.bias_heads > 1, dq);
-      if (ln.first && ln.head && ln.h0 == 0 && ed.in[u]) a.row_of[ed.to[u]] = (int32_t)row;
-      if (!ln.head) sum[u] = 0.f;
+      // (all lanes of a head write the same; lanes without an edge write to a spare place)
+      const int64_t to = ed.in[u] ? ed.to[u] : a.edges;
+#pragma unroll
+      for (int t = 0; t < RT; ++t) a.pd[to * a.heads + ln.h0 + t] = float2{p[t], ds[t]};
+      a.row_of[to] = (int32_t)row;
+      if (a.db && a.bias_heads > 1 && ed.in[u]) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) a.db[(g.e0 + ed.e[u]) * a.bias_heads + ln.h0 + t] = ds[t];
+      }
     }
     if (a.db && a.bias_heads == 1) {  // all heads are in the wave (else k_attend_grad_bias)
-      lanes_reduce<false>(sum, a.lg_g, a.lg_g + a.lg_h, AddF());
+#pragma unroll
+      for (int u = 0; u < U; ++u) sum[u] = ln.head ? sum[u] : 0.f;
+      lanes_reduce<false>(sum, Lane<T, V, RT, LG>::lg_g(a), Lane<T, V, RT, LG>::lg_g(a) + a.lg_h,
+                          AddF());
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (ln.first && ln.h0 == 0 && ln.head && ed.in[u]) a.db[g.e0 + ed.e[u]] = sum[u];
+        if (ed.in[u]) a.db[g.e0 + ed.e[u]] = sum[u];
     }
   }
-  const int from = a.lg_g + a.lg_h;
+  const int from = Lane<T, V, RT, LG>::lg_g(a) + a.lg_h;
 #pragma unroll
-  for (int t = 0; t < RT; ++t) lanes_reduce<false>(dq[t], from, from + lg_e, AddF());
+  for (int t = 0; t < RT; ++t) {
+    lanes_reduce<false>(dq[t], from, from + lg_e, AddF());
+    if (RT > 1) __builtin_amdgcn_sched_barrier(0);  // (a head at a time: fewer registers)
+  }
 }
 
-template <typename T, int V, int RT, int U>
-__global__ __launch_bounds__(AT, RT == 4 ? 2 : RT == 2 ? 3 : 4) void k_attend_grad_rows(Attend a) {
+template <typename T, int V, int RT, int U, int LG>
+__global__ __launch_bounds__(AT, RT == 1 ? 4 : 3) void k_attend_grad_rows(Attend a) {
   __shared__ Stage s_stage[AW];
-  typedef Lane<T, V, RT> L;
+  typedef Lane<T, V, RT, LG> L;
   bool bad = false;
   take_work<true, L>(
       a, &s_stage[__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))],
       [&](const L &ln, int64_t row, int start, int end, const Staged &g, int lg_e, int64_t slot) {
         float dq[RT][V];
-        grad_list<T, V, RT, U>(a, ln, row, g, start, end, lg_e, dq, &bad);
+        grad_list<T, V, RT, U, LG>(a, ln, row, g, start, end, lg_e, dq, &bad);
         if (slot == -2 || !ln.head || ln.es) return;
+        const int h0 = ln.head0();
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           if (slot >= 0) {
             Raw<float, V> r;
             memcpy(&r.w, dq[t], sizeof(dq[t]));
-            st_piece<false>(r, a.part + slot * a.slot + (ln.h0 + t) * a.D, ln.pc);
+            st_piece<false>(r, a.part + slot * a.slot + (h0 + t) * a.D, ln.pc);
             continue;
           }
           float y[V];
 #pragma unroll
           for (int i = 0; i < V; ++i) y[i] = dq[t][i] * a.scale;
           st_piece<false>(from_floats<T, V>(y),
-                          static_cast<T *>(a.dq) + (row * a.heads + ln.h0 + t) * a.D, ln.pc);
+                          static_cast<T *>(a.dq) + (row * a.heads + h0 + t) * a.D, ln.pc);
         }
       });
   if (bad && a.status) atomicOr(a.status, 1);
@@ -811,7 +868,7 @@ void set_lanes(Attend &a, int vec) {
   const int heads = log2_up(a.kv_heads);
   a.lg_h = heads < 6 - a.lg_g ? heads : 6 - a.lg_g;
   const int rest = 6 - a.lg_g - a.lg_h;
-  // edge slots for a list of middling length in one round of four edges a slot
+  // edge slots: one for about four edges of a middling list
   const int want = log2_up((a.edges / a.nq + 3) / 4);
   a.lg_e = want < rest ? want : rest;
   const int slots = 64 >> (a.lg_g + a.lg_h + a.lg_e);
@@ -829,12 +886,22 @@ bool heads_in_wave(const Attend &a, int rt) { return a.kv_heads <= 1 << a.lg_h &
 
 // Calls f(RT, U) with the query heads that a wave takes of each key head and the edges in
 // flight per lane.
-template <typename F>
+template <bool GRAD, typename F>
 void with_heads(int share, F f) {
   using std::integral_constant;
-  if (share % 4 == 0) f(integral_constant<int, 4>(), integral_constant<int, 2>());
-  else if (share % 2 == 0) f(integral_constant<int, 2>(), integral_constant<int, 4>());
-  else f(integral_constant<int, 1>(), integral_constant<int, 4>());
+  if (!GRAD && share % 4 == 0) f(integral_constant<int, GRAD ? 2 : 4>(), integral_constant<int, 1>());
+  else if (share % 2 == 0) f(integral_constant<int, 2>(), integral_constant<int, 2>());
+  else f(integral_constant<int, 1>(), integral_constant<int, 2>());
+}
+// Calls f(LG): heads of 4, 8 or 16 vectors (32 to 128 elements of 16 bits, 16 to 64 of 32)
+// get code of their own, whose steps among lanes need no branches.
+template <int V, typename F>
+void with_lanes(int lg_g, F f) {
+  using std::integral_constant;
+  if (V > 1 && lg_g == 2) f(integral_constant<int, V == 1 ? -1 : 2>());
+  else if (V > 1 && lg_g == 3) f(integral_constant<int, V == 1 ? -1 : 3>());
+  else if (V > 1 && lg_g == 4) f(integral_constant<int, V == 1 ? -1 : 4>());
+  else f(integral_constant<int, -1>());
 }
 dim3 attend_grid(const Attend &a, int rt) {
   const int tiles = (a.kv_heads + (1 << a.lg_h) - 1) >> a.lg_h;
@@ -1005,9 +1072,12 @@ extern "C" int dg_attend_edges(const void *q, int64_t q_stride, const void *k, i
     (void)with_vec<T>(D, [&](auto v) {
       constexpr int V = decltype(v)::value;
       set_lanes(a, V);
-      with_heads(a.share, [&](auto rt, auto u) {
-        hipLaunchKernelGGL((k_attend<T, V, decltype(rt)::value, decltype(u)::value>),
-                           attend_grid(a, decltype(rt)::value), dim3(AT), 0, stream, a);
+      with_heads<false>(a.share, [&](auto rt, auto u) {
+        with_lanes<V>(a.lg_g, [&](auto lg) {
+          hipLaunchKernelGGL(
+              (k_attend<T, V, decltype(rt)::value, decltype(u)::value, decltype(lg)::value>),
+              attend_grid(a, decltype(rt)::value), dim3(AT), 0, stream, a);
+        });
       });
       return (int)DG_OK;
     });
@@ -1028,8 +1098,8 @@ struct GradRoom {
 };
 GradRoom carve_grad(Carve &c, int64_t edges, int32_t heads, int32_t D) {
   GradRoom r;
-  r.pd = c.take<float2>((size_t)edges * (size_t)heads);
-  r.row_of = c.take<int32_t>((size_t)edges);
+  r.pd = c.take<float2>((size_t)(edges + 1) * (size_t)heads);
+  r.row_of = c.take<int32_t>((size_t)edges + 1);
   r.place = c.take<int32_t>((size_t)edges);
   r.part = c.take<char>(part_bytes(edges, (int64_t)heads * D));
   r.fixed = c.used;
@@ -1148,11 +1218,14 @@ extern "C" int dg_attend_edges_grad(
     (void)with_vec<T>(D, [&](auto v) {
       constexpr int V = decltype(v)::value;
       set_lanes(a, V);
-      with_heads(a.share, [&](auto rt, auto u) {
+      with_heads<true>(a.share, [&](auto rt, auto u) {
         all_heads = heads_in_wave(a, decltype(rt)::value);
         a.db = grad_bias && (all_heads || bias_heads > 1) ? grad_bias : nullptr;
-        hipLaunchKernelGGL((k_attend_grad_rows<T, V, decltype(rt)::value, decltype(u)::value>),
-                           attend_grid(a, decltype(rt)::value), dim3(AT), 0, stream, a);
+        with_lanes<V>(a.lg_g, [&](auto lg) {
+          hipLaunchKernelGGL((k_attend_grad_rows<T, V, decltype(rt)::value, decltype(u)::value,
+                                                 decltype(lg)::value>),
+                             attend_grid(a, decltype(rt)::value), dim3(AT), 0, stream, a);
+        });
       });
       launch_join<T, true>(a, stream);
       const int per = AT >> lanes.lg;
