@@ -544,6 +544,7 @@ __global__ __launch_bounds__(AT, RT == 1 ? 5 : 3) void k_attend(Attend a) {
 constexpr int JT = 1024;
 template <typename T, bool GRAD, int C>
 __global__ __launch_bounds__(JT) void k_attend_join(Attend a, int lg) {
+  constexpr int U = 12;  // parts in flight per lane
   __shared__ float s_m[JT / 64], s_acc[C][JT], s_l[JT];
   const int h = blockIdx.y;
   const int d = (threadIdx.x & ((1 << lg) - 1)) * C, g = threadIdx.x >> lg, groups = JT >> lg;
@@ -556,34 +557,32 @@ __global__ __launch_bounds__(JT) void k_attend_join(Attend a, int lg) {
     const int64_t start = a.offsets[row], end = a.offsets[row + 1];
     const int64_t first = 2 * c + (start > c * a.ch), parts = (end - 1) / a.ch - c + 1;
     auto part = [&](int64_t j) { return a.part + (j ? 2 * (c + j) : first) * a.slot; };
-    float top = NINF, from = 0.f;
-    if (!GRAD) {
-      for (int64_t j = threadIdx.x; j < parts; j += JT)
-        top = fmaxf(top, part(j)[a.heads * a.D + 2 * h]);
-      float t[1] = {top};
-      lanes_reduce<true>(t, 0, 6, MaxF());
-      if ((threadIdx.x & 63) == 0) s_m[threadIdx.x >> 6] = t[0];
-      __syncthreads();
-      top = NINF;
+    // each group keeps a running maximum of its own
+    float top = NINF, acc[C] = {}, sum = 0.f;
+    for (int64_t j0 = g; j0 < parts; j0 += U * groups) {
+      Raw<float, C> x[U];
+      float m[U], ls[U];
 #pragma unroll
-      for (int i = 0; i < JT / 64; ++i) top = fmaxf(top, s_m[i]);
-      from = top == NINF ? 0.f : top;
-    }
-    float acc[C] = {}, sum = 0.f;
-    for (int64_t j0 = g; j0 < parts; j0 += 8 * groups) {
-      Raw<float, C> x[8];
-      float m[8], ls[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < U; ++u) {
         const float *p = part(min(j0 + u * groups, parts - 1));
         x[u] = ld_raw<float, C>(p + h * a.D + min(d, a.D - C));
         m[u] = GRAD ? 0.f : p[a.heads * a.D + 2 * h];
         ls[u] = GRAD ? 0.f : p[a.heads * a.D + 2 * h + 1];
       }
+      if (!GRAD) {
+        float now = top;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+        for (int u = 0; u < U; ++u) now = fmaxf(now, m[u]);
+        const float f = now == NINF ? 1.f : exp_of(top - now);
+        top = now;
+        sum *= f;
+#pragma unroll
+        for (int i = 0; i < C; ++i) acc[i] *= f;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
         if (j0 + u * groups >= parts) continue;
-        const float f = GRAD ? 1.f : exp_of(m[u] - from);
+        const float f = GRAD ? 1.f : exp_of(m[u] - (top == NINF ? 0.f : top));
         if (f != 0.f) {
           float y[C];
           to_floats<float, C>(x[u], y);
@@ -592,6 +591,20 @@ __global__ __launch_bounds__(JT) void k_attend_join(Attend a, int lg) {
           sum += f * ls[u];
         }
       }
+    }
+    if (!GRAD) {
+      float t[1] = {top};
+      lanes_reduce<true>(t, 0, 6, MaxF());
+      if ((threadIdx.x & 63) == 0) s_m[threadIdx.x >> 6] = t[0];
+      __syncthreads();
+      float all = NINF;
+#pragma unroll
+      for (int i = 0; i < JT / 64; ++i) all = fmaxf(all, s_m[i]);
+      const float f = all == NINF ? 1.f : exp_of(top - all);
+      top = all;
+      sum *= f;
+#pragma unroll
+      for (int i = 0; i < C; ++i) acc[i] *= f;
     }
 #pragma unroll
     for (int i = 0; i < C; ++i) s_acc[i][threadIdx.x] = acc[i];

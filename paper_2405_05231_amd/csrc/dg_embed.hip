@@ -148,13 +148,15 @@ __global__ __launch_bounds__(ET) void k_embed_sum(IdSort a, uint32_t limit, cons
       });
 }
 
-// A block per long segment: its groups of lanes add every NG-th partial sum, then one
-// group adds theirs in order.
+constexpr int KT = 512;  // threads of a block of k_join
+
+// A block per long segment: its groups of lanes add every so many-th partial sum, then
+// each half of the groups its other half's.
 template <typename TO, int V>
-__global__ __launch_bounds__(ET) void k_join(IdSort a, JoinOut o, int cols, int lg) {
-  __shared__ float s_sum[ET * V];
+__global__ __launch_bounds__(KT) void k_join(IdSort a, JoinOut o, int cols, int lg) {
+  __shared__ float s_sum[KT * V];
   const int z = blockIdx.z;
-  const int sub = threadIdx.x & ((1 << lg) - 1), g = threadIdx.x >> lg, groups = ET >> lg;
+  const int sub = threadIdx.x & ((1 << lg) - 1), g = threadIdx.x >> lg, groups = KT >> lg;
   const Piece<V> pc((blockIdx.y << lg) + sub, cols);
   // (the grid is within the list's room)
   LongAt first = a.long_at[blockIdx.x];
@@ -169,11 +171,11 @@ __global__ __launch_bounds__(ET) void k_join(IdSort a, JoinOut o, int cols, int 
     {
       const int64_t at = lo + threadIdx.x;
       const int ok = __syncthreads_count(at < hi && a.dst[min(at, hi - 1) * a.C] == node);
-      if (ok < ET) hi = lo + ok;
+      if (ok < KT) hi = lo + ok;
       lo += ok - 1;
     }
     while (hi - lo > 1) {
-      const int64_t step = (hi - lo + ET - 1) / ET;
+      const int64_t step = (hi - lo + KT - 1) / KT;
       const int64_t at = lo + (int64_t)threadIdx.x * step;
       const int ok = __syncthreads_count(at < hi && a.dst[at * a.C] == node);
       lo += (int64_t)(ok - 1) * step;
@@ -199,16 +201,21 @@ __global__ __launch_bounds__(ET) void k_join(IdSort a, JoinOut o, int cols, int 
       }
     }
 #pragma unroll
-    for (int e = 0; e < V; ++e) s_sum[(e * groups + g) * (1 << lg) + sub] = acc[e];
+    for (int e = 0; e < V; ++e) s_sum[((e * groups + g) << lg) + sub] = acc[e];
     __syncthreads();
+    // halves of the groups, in the same order each time
+    for (int half = groups >> 1; half > 0; half >>= 1) {
+      if (g < half) {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          s_sum[((e * groups + g) << lg) + sub] += s_sum[((e * groups + g + half) << lg) + sub];
+      }
+      __syncthreads();
+    }
     if (g == 0) {
       float y[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        float t = 0.f;
-        for (int q = 0; q < groups; ++q) t += s_sum[(e * groups + q) * (1 << lg) + sub];
-        y[e] = t * o.factor[z];
-      }
+      for (int e = 0; e < V; ++e) y[e] = s_sum[((e * groups) << lg) + sub] * o.factor[z];
       st_piece<false>(from_floats<TO, V>(y),
                       static_cast<TO *>(o.out[z]) + (int64_t)node * o.stride[z], pc);
     }
@@ -248,7 +255,7 @@ int run_join(const IdSort &a, const JoinOut &o, int outs, int cols, int32_t type
       hipLaunchKernelGGL((k_join<TO, V>),
                          dim3((unsigned)(most > 512 ? 512 : most), (unsigned)r.tiles,
                               (unsigned)outs),
-                         dim3(ET), 0, s, a, o, cols, r.lg);
+                         dim3(KT), 0, s, a, o, cols, r.lg);
       DG_HIP(hipGetLastError());
       return (int)DG_OK;
     });

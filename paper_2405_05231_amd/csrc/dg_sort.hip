@@ -230,59 +230,98 @@ __global__ __launch_bounds__(ST) void k_heads_rank(IdSort a, const int32_t *key,
 }
 
 // ------------------------------------------------------------------ short lists
-// One block: keys and places as 64-bit numbers, sorted by exchanges in shared memory.
-constexpr int SMALL_T = 1024;
+// One block, 8 bits a pass: a wave holds 128 entries in a row, ranks them as
+// k_sort_place does, and the passes exchange them through shared memory.
+constexpr int SMALL_T = 1024, SMALL_W = SMALL_T / 64, SMALL_BITS = 8;
 __global__ __launch_bounds__(SMALL_T) void k_sort_small(IdSort a, int32_t *node_out,
                                                         int64_t *count, int32_t *status) {
-  __shared__ uint64_t s[SMALL];
-  const int n = (int)a.n;
-  int size = 2;
-  while (size < n) size <<= 1;
+  constexpr int R = SMALL / SMALL_T, SB = 1 << SMALL_BITS;
+  __shared__ uint32_t s_at[SMALL_W][SB];
+  __shared__ int2 s[SMALL];
+  __shared__ int32_t s_sum[SB / 64];
+  const int n = (int)a.n, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const uint64_t lt = lanes_below();
+  int2 x[R];
   bool bad = false;
-  for (int i = threadIdx.x; i < size; i += SMALL_T) {
-    const int32_t k = i < n ? sort_key(a.ids[i], a.slots, &bad) : -1;
-    s[i] = i < n ? (uint64_t)(uint32_t)k << 32 | (uint32_t)i : ~0ull;
-    if (!a.compact && i < n && k < a.slots) a.seen[k] = 1;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int i = w * (64 * R) + r * 64 + lane;
+    x[r] = int2{i < n ? sort_key(a.ids[i], a.slots, &bad) : 0, i};
+    if (!a.compact && i < n && x[r].x < a.slots) a.seen[x[r].x] = 1;
   }
   if (bad && status) atomicOr(status, 1);
   if (threadIdx.x == 0) *a.n_long = 0;
-  for (int run = 2; run <= size; run <<= 1) {
-    for (int step = run >> 1; step > 0; step >>= 1) {
-      __syncthreads();
-      const int t = threadIdx.x;
-      if (t < size / 2) {
-        const int i = 2 * t - (t & (step - 1)), j = i + step;
-        const uint64_t x = s[i], y = s[j];
-        if ((x > y) == ((i & run) == 0)) {
-          s[i] = y;
-          s[j] = x;
-        }
+  for (int shift = 0; a.slots >> shift; shift += SMALL_BITS) {
+    for (int i = threadIdx.x; i < SMALL_W * SB; i += SMALL_T) (&s_at[0][0])[i] = 0;
+    __syncthreads();
+    uint32_t rank[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool in = w * (64 * R) + r * 64 + lane < n;
+      const uint32_t d = ((uint32_t)x[r].x >> shift) & (SB - 1);
+      const uint64_t same = same_digit(d, SMALL_BITS, __ballot(in));
+      rank[r] = 0;
+      if (in) {
+        const uint32_t old = s_at[w][d];
+        rank[r] = old + __popcll(same & lt);
+        __builtin_amdgcn_wave_barrier();
+        if (__builtin_ctzll(same) == lane) s_at[w][d] = old + (uint32_t)__popcll(same);
       }
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    // each digit's entries before each wave's, then before each digit's
+    int32_t mine = 0, incl = 0;
+    if (threadIdx.x < SB) {
+#pragma unroll
+      for (int j = 0; j < SMALL_W; ++j) {
+        const uint32_t v = s_at[j][threadIdx.x];
+        s_at[j][threadIdx.x] = (uint32_t)mine;
+        mine += (int32_t)v;
+      }
+      incl = wave_incl_sum_i32(mine);
+      if (lane == 63) s_sum[w] = incl;
+    }
+    __syncthreads();
+    if (threadIdx.x < SB) {
+      int32_t before = incl - mine;
+      for (int j = 0; j < w; ++j) before += s_sum[j];
+#pragma unroll
+      for (int j = 0; j < SMALL_W; ++j) s_at[j][threadIdx.x] += (uint32_t)before;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (w * (64 * R) + r * 64 + lane < n)
+        s[s_at[w][((uint32_t)x[r].x >> shift) & (SB - 1)] + rank[r]] = x[r];
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int i = w * (64 * R) + r * 64 + lane;
+      if (i < n) x[r] = s[i];
     }
   }
-  __syncthreads();
-  // SMALL / SMALL_T entries in a row per thread
-  constexpr int PER = SMALL / SMALL_T;
-  bool head[PER];
+  // R entries in a row per thread
+  bool head[R];
   int mine = 0;
 #pragma unroll
-  for (int r = 0; r < PER; ++r) {
-    const int i = threadIdx.x * PER + r;
-    const int32_t k = i < n ? (int32_t)(s[i] >> 32) : -1;
-    head[r] = i < n && k < a.slots && (i == 0 || (int32_t)(s[i - 1] >> 32) != k);
+  for (int r = 0; r < R; ++r) {
+    const int i = threadIdx.x * R + r;
+    const int32_t k = i < n ? s[i].x : -1;
+    head[r] = i < n && k < a.slots && (i == 0 || s[i - 1].x != k);
     mine += head[r];
   }
-  int64_t all = 0;
-  int64_t at = block_excl_scan<SMALL_T>(mine, &all) - 1;
+  int64_t all = 0, at = 0;
+  if (a.compact) at = block_excl_scan<SMALL_T>(mine, &all) - 1;
   if (a.compact && threadIdx.x == 0) *count = all;
 #pragma unroll
-  for (int r = 0; r < PER; ++r) {
-    const int i = threadIdx.x * PER + r;
+  for (int r = 0; r < R; ++r) {
+    const int i = threadIdx.x * R + r;
     if (i >= n) break;
-    const int32_t k = (int32_t)(s[i] >> 32);
+    const int32_t k = s[i].x;
     at += head[r];
-    if (a.place) a.place[(uint32_t)s[i]] = i;
-    else a.order[i] = (int32_t)(uint32_t)s[i];
+    if (a.place) a.place[s[i].y] = i;
+    else a.order[i] = s[i].y;
     a.dst[i] = !a.compact ? k : k < a.slots ? (int32_t)at : -1;
     if (a.compact && head[r]) node_out[at] = k;
   }
