@@ -232,6 +232,8 @@ __global__ __launch_bounds__(ST) void k_heads_rank(IdSort a, const int32_t *key,
 // ------------------------------------------------------------------ short lists
 // One block, 8 bits a pass: a wave holds 128 entries in a row, ranks them as
 // k_sort_place does, and the passes exchange them through shared memory.
+// tables whose marks that block clears by itself, which is worth a launch
+constexpr int64_t SMALL_SEEN = 1 << 17;
 constexpr int SMALL_T = 1024, SMALL_W = SMALL_T / 64, SMALL_BITS = 8;
 __global__ __launch_bounds__(SMALL_T) void k_sort_small(IdSort a, int32_t *node_out,
                                                         int64_t *count, int32_t *status) {
@@ -243,6 +245,11 @@ __global__ __launch_bounds__(SMALL_T) void k_sort_small(IdSort a, int32_t *node_
   const uint64_t lt = lanes_below();
   int2 x[R];
   bool bad = false;
+  if (!a.compact && a.slots <= SMALL_SEEN) {  // else run_sort has cleared them
+    for (int64_t i = threadIdx.x; i < (a.slots + 15) / 16; i += SMALL_T)
+      reinterpret_cast<uint4 *>(a.seen)[i] = uint4{0, 0, 0, 0};
+    __syncthreads();
+  }
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int i = w * (64 * R) + r * 64 + lane;
@@ -371,7 +378,7 @@ size_t sort_room(IdSort a) {
 }
 
 int run_sort(IdSort &a, int32_t *node_out, int64_t *count, int32_t *status, hipStream_t s) {
-  if (!a.compact) {
+  if (!a.compact && (a.n == 0 || a.n > SMALL || a.slots > SMALL_SEEN)) {
     // (carved in pieces of 256 bytes, so whole words hold it)
     DG_TRY(fill_u64((uint64_t *)a.seen, (size_t)(a.slots + 7) / 8, 0, s));
   }

@@ -9,7 +9,7 @@ of range and 2 for offsets out of order; such entries add nothing.
 """
 from __future__ import annotations
 
-import contextlib
+import functools
 from dataclasses import dataclass
 
 import torch
@@ -24,11 +24,23 @@ _TYPES = {torch.float32: _lib.DG_F32, torch.float16: _lib.DG_F16, torch.bfloat16
 _WIDE = (torch.float32, torch.float16, torch.bfloat16)
 
 
-def _on(stream):
-    """(context that makes allocations on the stream, its handle)."""
-    if stream is None:
-        return contextlib.nullcontext(), torch.cuda.current_stream().cuda_stream
-    return torch.cuda.stream(stream), stream.cuda_stream
+# Handle of the current stream of a device.  torch's own query is used without the Stream
+# object around it where it is there: small calls are bound by such costs (2.8 us of the
+# 13 us that a lookup of one row took).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                      lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _on_stream(f):
+    """Lets f(..., stream=s) run with s as the current stream, so that what it allocates
+    belongs to s."""
+    @functools.wraps(f)
+    def call(*args, stream=None, **kw):
+        if stream is None:
+            return f(*args, **kw)
+        with torch.cuda.stream(stream):
+            return f(*args, **kw)
+    return call
 
 
 def _gpu(t, name: str, dtypes, device=None):
@@ -43,31 +55,39 @@ def _gpu(t, name: str, dtypes, device=None):
 
 
 def _whole(t, name: str, dtype, device, numel=None):
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_contiguous()
+            and t.device == device and t.is_cuda and (numel is None or t.numel() == numel)):
+        return
     _gpu(t, name, (dtype,), device)
     if not t.is_contiguous():
         raise ValueError(f"{name}: must be contiguous")
-    if numel is not None and t.numel() != numel:
-        raise ValueError(f"{name}: expected {numel} elements, got {t.numel()}")
+    raise ValueError(f"{name}: expected {numel} elements, got {t.numel()}")
 
 
 def _rows(t, name: str, dtypes, device=None, shape=None, dims: int = 2) -> int:
     """Checks a tensor of rows (the elements of a row adjacent, rows apart by any stride)
     and returns the stride of its rows."""
     _gpu(t, name, dtypes, device)
-    if t.dim() != dims:
-        raise ValueError(f"{name}: expected {dims} dimensions, got {t.dim()}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    width = 1
+    have = t.shape
+    if len(have) != dims:
+        raise ValueError(f"{name}: expected {dims} dimensions, got {len(have)}")
+    if shape is not None and have != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(have)}")
+    stride, width = t.stride(), 1
     for d in range(dims - 1, 0, -1):
-        if t.shape[d] != 1 and t.stride(d) != width:
+        if stride[d] != width and have[d] != 1:
             raise ValueError(f"{name}: the elements of a row must be adjacent")
-        width *= t.shape[d]
-    if t.shape[0] <= 1:
+        width *= have[d]
+    if have[0] <= 1:
         return max(width, 1)
-    if t.stride(0) < width:
+    if stride[0] < width:
         raise ValueError(f"{name}: rows must not overlap")
-    return t.stride(0)
+    return stride[0]
+
+
+def _like(t):
+    """A contiguous tensor of t's shape, type and device."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
 
 
 def _out(t, name: str, shape, dtype, device):
@@ -84,9 +104,10 @@ def _ptr(t):
 
 
 def _status(t, device):
-    if t is not None:
-        _whole(t, "status", torch.int32, device, 1)
-    return _ptr(t)
+    if t is None:
+        return None
+    _whole(t, "status", torch.int32, device, 1)
+    return t.data_ptr()
 
 
 def _workspace(nbytes: int, device, ws):
@@ -99,10 +120,10 @@ def _workspace(nbytes: int, device, ws):
 
 
 # ------------------------------------------------------------------------ embedding rows
+@_on_stream
 def embed_rows(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
                row_scale: torch.Tensor | None = None, dtype: torch.dtype | None = None,
-               out: torch.Tensor | None = None, status: torch.Tensor | None = None,
-               stream=None) -> torch.Tensor:
+               out: torch.Tensor | None = None, status: torch.Tensor | None = None) -> torch.Tensor:
     """Rows of a learned table (dg_embed_rows): out[i] = scale * row_scale[ids[i]] *
     table[ids[i]].  table: [N, D] in float32, float16, bfloat16 or float8_e4m3fn; ids:
     int32 [n], -1 for a zero row; row_scale: float32 [N], for tables in 8 bits.  dtype:
@@ -119,21 +140,21 @@ def embed_rows(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
     if dtype not in _WIDE:
         raise TypeError(f"dtype: expected float32, float16 or bfloat16, got {dtype}")
     n = ids.numel()
-    on, s = _on(stream)
-    with on:
-        if out is None:
-            out = torch.empty((n, D), dtype=dtype, device=dev)
+    if out is None:
+        out, out_stride = torch.empty((n, D), dtype=dtype, device=dev), D
+    else:
         out_stride = _rows(out, "out", (dtype,), dev, (n, D))
-        check(_L.dg_embed_rows(_ptr(table), _TYPES[table.dtype], N, D, stride, _ptr(row_scale),
-                               _ptr(ids), n, scale, _ptr(out), _TYPES[dtype], out_stride,
-                               _status(status, dev), s))
+    check(_L.dg_embed_rows(_ptr(table), _TYPES[table.dtype], N, D, stride, _ptr(row_scale),
+                           _ptr(ids), n, scale, _ptr(out), _TYPES[dtype], out_stride,
+                           _status(status, dev), _raw_stream(dev.index)))
     return out
 
 
+@_on_stream
 def embed_rows_grad(grad_out: torch.Tensor, ids: torch.Tensor, num_rows: int, scale: float = 1.0,
                     sparse: bool = False, dtype: torch.dtype | None = None,
                     out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
-                    status: torch.Tensor | None = None, stream=None):
+                    status: torch.Tensor | None = None):
     """Gradient of embed_rows towards a table of num_rows rows (dg_embed_rows_grad): for
     each node the sum of scale * grad_out over the list entries that hold it, in list
     order.  Returns the whole gradient [num_rows, D], or with sparse=True (nodes int32
@@ -148,22 +169,21 @@ def embed_rows_grad(grad_out: torch.Tensor, ids: torch.Tensor, num_rows: int, sc
     if dtype not in _WIDE:
         raise TypeError(f"dtype: expected float32, float16 or bfloat16, got {dtype}")
     most = min(n, num_rows) if sparse else num_rows
-    on, s = _on(stream)
-    with on:
-        grad = _out(out, "out", (most, D), dtype, dev)
-        nodes = count = None
-        if sparse:
-            nodes = torch.empty(max(most, 1), dtype=torch.int32, device=dev)
-            count = torch.empty(1, dtype=torch.int64, device=dev)
-        ws, ws_bytes = _workspace(
-            _L.dg_embed_rows_grad_workspace_bytes(num_rows, D, n, int(sparse)), dev, workspace)
-        check(_L.dg_embed_rows_grad(_ptr(grad_out), _TYPES[grad_out.dtype], stride, _ptr(ids), n,
-                                    num_rows, D, scale, _ptr(grad), _TYPES[dtype], _ptr(nodes),
-                                    _ptr(count), _status(status, dev), _ptr(ws), ws_bytes, s))
-        if not sparse:
-            return grad
-        u = int(count)
-        return nodes[:u], grad[:u]
+    grad = _out(out, "out", (most, D), dtype, dev)
+    nodes = count = None
+    if sparse:
+        nodes = torch.empty(max(most, 1), dtype=torch.int32, device=dev)
+        count = torch.empty(1, dtype=torch.int64, device=dev)
+    ws, ws_bytes = _workspace(
+        _L.dg_embed_rows_grad_workspace_bytes(num_rows, D, n, int(sparse)), dev, workspace)
+    check(_L.dg_embed_rows_grad(_ptr(grad_out), _TYPES[grad_out.dtype], stride, _ptr(ids), n,
+                                num_rows, D, scale, _ptr(grad), _TYPES[dtype], _ptr(nodes),
+                                _ptr(count), _status(status, dev), _ptr(ws), ws_bytes,
+                                _raw_stream(dev.index)))
+    if not sparse:
+        return grad
+    u = int(count)
+    return nodes[:u], grad[:u]
 
 
 # ------------------------------------------------------------------------ RMS norm
@@ -175,9 +195,9 @@ class NormResult:
     rstd: torch.Tensor          # float32 [n]
 
 
+@_on_stream
 def norm_rows(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | None = None,
-              eps: float = 1e-6, dtype: torch.dtype | None = None, group: int = 0,
-              stream=None) -> NormResult:
+              eps: float = 1e-6, dtype: torch.dtype | None = None, group: int = 0) -> NormResult:
     """RMS norm of the rows of x + residual, times weight (dg_norm_rows).  dtype: the
     type of y, x's own (by default) or float8_e4m3fn, with one scale per row (group = 0)
     or per group of 32, 64 or 128 columns."""
@@ -192,24 +212,22 @@ def norm_rows(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | No
         dtype = x.dtype
     if dtype not in _TYPES:
         raise TypeError(f"dtype: expected {x.dtype} or torch.float8_e4m3fn, got {dtype}")
-    on, s = _on(stream)
-    with on:
-        y = torch.empty((n, D), dtype=dtype, device=dev)
-        rstd = torch.empty(n, dtype=torch.float32, device=dev)
-        h = torch.empty((n, D), dtype=x.dtype, device=dev) if residual is not None else None
-        scales = None
-        if dtype == torch.float8_e4m3fn:
-            groups = -(-D // group) if group > 0 else 1
-            scales = torch.empty((n, groups), dtype=torch.float32, device=dev)
-        check(_L.dg_norm_rows(_ptr(x), stride, _ptr(residual), res_stride, _TYPES[x.dtype], n, D,
-                              _ptr(weight), eps, _ptr(y), _TYPES[dtype], group, _ptr(scales),
-                              _ptr(h), _ptr(rstd), s))
+    y = _like(x) if dtype is x.dtype else torch.empty((n, D), dtype=dtype, device=dev)
+    rstd = torch.empty(n, dtype=torch.float32, device=dev)
+    h = _like(x) if residual is not None else None
+    scales = None
+    if dtype == torch.float8_e4m3fn:
+        groups = -(-D // group) if group > 0 else 1
+        scales = torch.empty((n, groups), dtype=torch.float32, device=dev)
+    check(_L.dg_norm_rows(_ptr(x), stride, _ptr(residual), res_stride, _TYPES[x.dtype], n, D,
+                          _ptr(weight), eps, _ptr(y), _TYPES[dtype], group, _ptr(scales),
+                          _ptr(h), _ptr(rstd), _raw_stream(dev.index)))
     return NormResult(y, scales, x if h is None else h, rstd)
 
 
+@_on_stream
 def norm_rows_grad(grad_y: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, weight: torch.Tensor,
-                   grad_h: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
-                   stream=None):
+                   grad_h: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     """Gradient of norm_rows (dg_norm_rows_grad), from its h and rstd: (grad_x [n, D], which
     is the residual's gradient too, grad_weight float32 [D]).  grad_h: the gradient that
     reaches h by itself.  An 8-bit y counts as y before its rounding."""
@@ -222,14 +240,12 @@ def norm_rows_grad(grad_y: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, we
     gh_stride = 0
     if grad_h is not None:
         gh_stride = _rows(grad_h, "grad_h", (grad_y.dtype,), dev, (n, D))
-    on, s = _on(stream)
-    with on:
-        gx = torch.empty((n, D), dtype=grad_y.dtype, device=dev)
-        gw = torch.empty(D, dtype=torch.float32, device=dev)
-        ws, ws_bytes = _workspace(_L.dg_norm_rows_grad_workspace_bytes(n, D), dev, workspace)
-        check(_L.dg_norm_rows_grad(_ptr(grad_y), stride, _ptr(h), h_stride, _ptr(rstd),
-                                   _ptr(weight), _ptr(grad_h), gh_stride, _TYPES[grad_y.dtype], n,
-                                   D, _ptr(gx), _ptr(gw), _ptr(ws), ws_bytes, s))
+    gx, gw = _like(grad_y), torch.empty_like(weight)
+    ws, ws_bytes = _workspace(_L.dg_norm_rows_grad_workspace_bytes(n, D), dev, workspace)
+    check(_L.dg_norm_rows_grad(_ptr(grad_y), stride, _ptr(h), h_stride, _ptr(rstd),
+                               _ptr(weight), _ptr(grad_h), gh_stride, _TYPES[grad_y.dtype], n,
+                               D, _ptr(gx), _ptr(gw), _ptr(ws), ws_bytes,
+                               _raw_stream(dev.index)))
     return gx, gw
 
 
@@ -248,17 +264,16 @@ class AttendGrads:
     bias: torch.Tensor | None
 
 
+@_on_stream
 def edge_offsets(edge_src: torch.Tensor, num_rows: int, out: torch.Tensor | None = None,
-                 status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+                 status: torch.Tensor | None = None) -> torch.Tensor:
     """Offsets int64 [num_rows + 1] of an edge list sorted by row (dg_edge_offsets), as
     sample_group lists a mini-batch's edges by edge_src."""
     dev = edge_src.device if isinstance(edge_src, torch.Tensor) else None
     _whole(edge_src, "edge_src", torch.int32, dev)
-    on, s = _on(stream)
-    with on:
-        out = _out(out, "out", (num_rows + 1,), torch.int64, dev)
-        check(_L.dg_edge_offsets(_ptr(edge_src), edge_src.numel(), num_rows, _ptr(out),
-                                 _status(status, dev), s))
+    out = _out(out, "out", (num_rows + 1,), torch.int64, dev)
+    check(_L.dg_edge_offsets(_ptr(edge_src), edge_src.numel(), num_rows, _ptr(out),
+                             _status(status, dev), _raw_stream(dev.index)))
     return out
 
 
@@ -283,10 +298,11 @@ def _attend_args(q, k, v, offsets, indices, bias):
     return dev, qs, ks, vs, nq, nkv, heads, kv_heads, D, edges, bias_heads
 
 
+@_on_stream
 def attend_edges(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor,
                  indices: torch.Tensor, scale: float | None = None,
                  bias: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
-                 status: torch.Tensor | None = None, stream=None) -> AttendResult:
+                 status: torch.Tensor | None = None) -> AttendResult:
     """Attention of rows over lists of neighbours (dg_attend_edges): row i of q [nq, heads,
     D] attends over rows indices[offsets[i]:offsets[i + 1]] of k and v [nkv, kv_heads, D];
     heads is a multiple of kv_heads.  offsets int64 [nq + 1], indices int32 [edges] (-1: no
@@ -294,25 +310,24 @@ def attend_edges(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: tor
     masked edge.  scale: 1/sqrt(D) by default."""
     dev, qs, ks, vs, nq, nkv, heads, kv_heads, D, edges, bias_heads = _attend_args(
         q, k, v, offsets, indices, bias)
-    on, s = _on(stream)
-    with on:
-        out = torch.empty((nq, heads, D), dtype=q.dtype, device=dev)
-        lse = torch.empty((nq, heads), dtype=torch.float32, device=dev)
-        ws, ws_bytes = _workspace(_L.dg_attend_edges_workspace_bytes(edges, heads, D), dev,
-                                  workspace)
-        check(_L.dg_attend_edges(_ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _TYPES[q.dtype], nq, nkv,
-                                 heads, kv_heads, D, _ptr(offsets), _ptr(indices), edges,
-                                 _ptr(bias), bias_heads, D ** -0.5 if scale is None else scale,
-                                 _ptr(out), _ptr(lse), _status(status, dev), _ptr(ws), ws_bytes,
-                                 s))
+    out = _like(q)
+    lse = torch.empty((nq, heads), dtype=torch.float32, device=dev)
+    ws, ws_bytes = _workspace(_L.dg_attend_edges_workspace_bytes(edges, heads, D), dev,
+                              workspace)
+    check(_L.dg_attend_edges(_ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _TYPES[q.dtype], nq, nkv,
+                             heads, kv_heads, D, _ptr(offsets), _ptr(indices), edges,
+                             _ptr(bias), bias_heads, D ** -0.5 if scale is None else scale,
+                             _ptr(out), _ptr(lse), _status(status, dev), _ptr(ws), ws_bytes,
+                             _raw_stream(dev.index)))
     return AttendResult(out, lse)
 
 
+@_on_stream
 def attend_edges_grad(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                       out: torch.Tensor, lse: torch.Tensor, offsets: torch.Tensor,
                       indices: torch.Tensor, scale: float | None = None,
                       bias: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
-                      status: torch.Tensor | None = None, stream=None) -> AttendGrads:
+                      status: torch.Tensor | None = None) -> AttendGrads:
     """Gradient of attend_edges (dg_attend_edges_grad) from its results out and lse; the
     probabilities are recomputed.  Sums over shared keys run in a fixed order."""
     dev, qs, ks, vs, nq, nkv, heads, kv_heads, D, edges, bias_heads = _attend_args(
@@ -320,17 +335,13 @@ def attend_edges_grad(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, 
     gs = _rows(grad_out, "grad_out", (q.dtype,), dev, tuple(q.shape), dims=3)
     os_ = _rows(out, "out", (q.dtype,), dev, tuple(q.shape), dims=3)
     _whole(lse, "lse", torch.float32, dev, nq * heads)
-    on, s = _on(stream)
-    with on:
-        gq = torch.empty((nq, heads, D), dtype=q.dtype, device=dev)
-        gk = torch.empty((nkv, kv_heads, D), dtype=q.dtype, device=dev)
-        gv = torch.empty((nkv, kv_heads, D), dtype=q.dtype, device=dev)
-        gb = torch.empty(bias.shape, dtype=torch.float32, device=dev) if bias is not None else None
-        ws, ws_bytes = _workspace(
-            _L.dg_attend_edges_grad_workspace_bytes(edges, nkv, heads, kv_heads, D), dev, workspace)
-        check(_L.dg_attend_edges_grad(
-            _ptr(grad_out), gs, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(out), os_, _ptr(lse),
-            _TYPES[q.dtype], nq, nkv, heads, kv_heads, D, _ptr(offsets), _ptr(indices), edges,
-            _ptr(bias), bias_heads, D ** -0.5 if scale is None else scale, _ptr(gq), _ptr(gk),
-            _ptr(gv), _ptr(gb), _status(status, dev), _ptr(ws), ws_bytes, s))
+    gq, gk, gv = _like(q), _like(k), _like(v)
+    gb = torch.empty_like(bias) if bias is not None else None
+    ws, ws_bytes = _workspace(
+        _L.dg_attend_edges_grad_workspace_bytes(edges, nkv, heads, kv_heads, D), dev, workspace)
+    check(_L.dg_attend_edges_grad(
+        _ptr(grad_out), gs, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(out), os_, _ptr(lse),
+        _TYPES[q.dtype], nq, nkv, heads, kv_heads, D, _ptr(offsets), _ptr(indices), edges,
+        _ptr(bias), bias_heads, D ** -0.5 if scale is None else scale, _ptr(gq), _ptr(gk),
+        _ptr(gv), _ptr(gb), _status(status, dev), _ptr(ws), ws_bytes, _raw_stream(dev.index)))
     return AttendGrads(gq, gk, gv, gb)
