@@ -757,7 +757,7 @@ __global__ __launch_bounds__(AT, RT == 1 ? 4 : 3) void k_attend_grad_rows(Attend
 template <typename T, int V>
 __global__ __launch_bounds__(AT) void k_attend_grad_keys(Attend a, IdSort so, T *dk, T *dv, int vph,
                                                          int64_t sum_blocks) {
-  constexpr int U = 4;
+  constexpr int U = 2;
   extern __shared__ int2 s_entries[];
   const int lg = so.lg, sub = threadIdx.x & ((1 << lg) - 1), g = threadIdx.x >> lg;
   const int per = AT >> lg;
