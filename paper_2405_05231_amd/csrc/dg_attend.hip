@@ -539,7 +539,9 @@ __global__ __launch_bounds__(AT, RT == 1 ? 5 : 3) void k_attend(Attend a) {
 }
 
 // Joins the partial results of the long lists, a list at a time: groups of 2^lg lanes take
-// every such part, C columns a lane.  A block looks through 64 chunks for those in which a
+// every such part, C columns a lane, C * 2^lg columns of a head a block (one block for a head
+// is bound by its loads: 719,000 edges, 2809 parts of 8 x 64 columns, 21 us with 64 columns a
+// block and JOIN_US with 16).  A block looks through 64 chunks for those in which a
 // list starts, so that a call without long lists pays for few blocks.
 constexpr int JT = 1024;
 template <typename T, bool GRAD, int C>
@@ -547,7 +549,8 @@ __global__ __launch_bounds__(JT) void k_attend_join(Attend a, int lg) {
   constexpr int U = 12;  // parts in flight per lane
   __shared__ float s_m[JT / 64], s_acc[C][JT], s_l[JT];
   const int h = blockIdx.y;
-  const int d = (threadIdx.x & ((1 << lg) - 1)) * C, g = threadIdx.x >> lg, groups = JT >> lg;
+  const int d = ((blockIdx.z << lg) + (threadIdx.x & ((1 << lg) - 1))) * C;
+  const int g = threadIdx.x >> lg, groups = JT >> lg;
   const int64_t c0 = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
   uint64_t todo = __ballot(c0 < a.chunks && a.starts[min(c0, a.chunks - 1)] >= 0);
   while (todo) {  // the same for the block
@@ -566,8 +569,12 @@ __global__ __launch_bounds__(JT) void k_attend_join(Attend a, int lg) {
       for (int u = 0; u < U; ++u) {
         const float *p = part(min(j0 + u * groups, parts - 1));
         x[u] = ld_raw<float, C>(p + h * a.D + min(d, a.D - C));
-        m[u] = GRAD ? 0.f : p[a.heads * a.D + 2 * h];
-        ls[u] = GRAD ? 0.f : p[a.heads * a.D + 2 * h + 1];
+        if (!GRAD) {
+          float y[2];
+          to_floats<float, 2>(ld_raw<float, 2>(p + a.heads * a.D + 2 * h), y);
+          m[u] = y[0];
+          ls[u] = y[1];
+        }
       }
       if (!GRAD) {
         float now = top;
@@ -588,7 +595,7 @@ __global__ __launch_bounds__(JT) void k_attend_join(Attend a, int lg) {
           to_floats<float, C>(x[u], y);
 #pragma unroll
           for (int i = 0; i < C; ++i) acc[i] += f * y[i];
-          sum += f * ls[u];
+          if (!GRAD) sum += f * ls[u];
         }
       }
     }
@@ -925,9 +932,11 @@ dim3 attend_grid(const Attend &a, int rt) {
 template <typename T, bool GRAD>
 void launch_join(const Attend &a, hipStream_t s) {
   if (!a.chunks) return;
-  const dim3 g((unsigned)((a.chunks + 63) / 64), (unsigned)a.heads);
+  const int tiles = a.D % 16 == 0 ? a.D / 16 : 1;
+  const dim3 g((unsigned)((a.chunks + 63) / 64), (unsigned)a.heads, (unsigned)tiles);
   if (a.D % 4 == 0)
-    hipLaunchKernelGGL((k_attend_join<T, GRAD, 4>), g, dim3(JT), 0, s, a, log2_up(a.D / 4));
+    hipLaunchKernelGGL((k_attend_join<T, GRAD, 4>), g, dim3(JT), 0, s, a,
+                       log2_up(a.D / 4 / tiles));
   else
     hipLaunchKernelGGL((k_attend_join<T, GRAD, 1>), g, dim3(JT), 0, s, a, log2_up(a.D));
 }

@@ -183,16 +183,16 @@ __global__ __launch_bounds__(KT) void k_join(IdSort a, JoinOut o, int cols, int 
     }
     const int64_t parts = lo - c + 1;
     float acc[V] = {};
-    for (int64_t j0 = g; j0 < parts; j0 += 4 * groups) {
-      Raw<float, V> x[4];
+    for (int64_t j0 = g; j0 < parts; j0 += 8 * groups) {
+      Raw<float, V> x[8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < 8; ++u) {
         const int64_t j = min(j0 + u * groups, parts - 1);
         const int64_t slot = j == 0 ? 2 * c + 1 : 2 * (c + j);
         x[u] = ld_piece<float, V>(a.part + slot * a.width + o.at[z], pc);
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < 8; ++u) {
         if (j0 + u * groups >= parts) continue;
         float y[V];
         to_floats<float, V>(x[u], y);
