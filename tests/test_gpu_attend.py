@@ -534,3 +534,13 @@ def test_in_a_graph(dg):
         torch.cuda.synchronize()
         for x, y in zip(outs, want):
             assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("heads,kv_heads,D", [(1, 1, 3), (8, 2, 64), (6, 2, 50), (20, 20, 40),
+                                              (12, 3, 256), (3, 1, 16), (16, 8, 128)])
+def test_long_lists_with_every_head_layout(dg, dtype, heads, kv_heads, D):
+    """Lists cut into chunks where a wave holds some of the heads, all of them, or several
+    query heads of a key head."""
+    p = problem([2, 700, 0, 5, 131, 1], 90, heads, kv_heads, D, dtype, "edge")
+    check_gradient(dg, p, check_forward(dg, p))

@@ -254,3 +254,29 @@ def test_refusals(dg):
         dg.norm_rows_grad(x, x, randn(1, 3), w)
     with pytest.raises(TypeError):
         dg.norm_rows_grad(x, x.half(), randn(1, 4), w)
+
+
+@pytest.mark.parametrize("D", [3, 100, 768, 5000])
+def test_outputs_may_replace_inputs(dg, D):
+    """h in place of x or of the residual, grad_x in place of grad_y or of grad_h, through the
+    C ABI: the same bits as with outputs of their own."""
+    L, n = dg._L, 300
+    x, res, w = randn(1, n, D), randn(2, n, D), randn(3, D)
+    s = torch.cuda.current_stream().cuda_stream
+    want = dg.norm_rows(x, w, residual=res)
+    for place in ("x", "res"):
+        a, b = x.clone(), res.clone()
+        h, y, rstd = (a if place == "x" else b), torch.empty_like(x), torch.empty(n, device=DEV)
+        assert L.dg_norm_rows(a.data_ptr(), D, b.data_ptr(), D, 0, n, D, w.data_ptr(), 1e-6,
+                              y.data_ptr(), 0, 0, None, h.data_ptr(), rstd.data_ptr(), s) == 0
+        assert torch.equal(h, want.h) and torch.equal(y, want.y) and torch.equal(rstd, want.rstd)
+    gy, gh = randn(4, n, D), randn(5, n, D)
+    want_x, want_w = dg.norm_rows_grad(gy, want.h, want.rstd, w, grad_h=gh)
+    ws = torch.empty(L.dg_norm_rows_grad_workspace_bytes(n, D), dtype=torch.uint8, device=DEV)
+    for place in ("gy", "gh"):
+        a, b, gw = gy.clone(), gh.clone(), torch.empty_like(w)
+        gx = a if place == "gy" else b
+        assert L.dg_norm_rows_grad(a.data_ptr(), D, want.h.data_ptr(), D, want.rstd.data_ptr(),
+                                   w.data_ptr(), b.data_ptr(), D, 0, n, D, gx.data_ptr(),
+                                   gw.data_ptr(), ws.data_ptr(), ws.numel(), s) == 0
+        assert torch.equal(gx, want_x) and torch.equal(gw, want_w)
