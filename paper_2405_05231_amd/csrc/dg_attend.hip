@@ -758,12 +758,12 @@ __global__ __launch_bounds__(AT, RT == 1 ? 4 : 3) void k_attend_grad_rows(Attend
 
 // ------------------------------------------------------------------ gradient by keys
 // A group of 2^lg lanes per chunk of the edges in the order of their keys, each lane a
-// vector of one key head (vph vectors per head); blocks from sum_blocks on write the
-// rows of keys without an edge as zeros.  The steps are the edges' query heads: `share`
+// vector of one key head (vph vectors per head); the first zero_blocks write the rows of
+// keys without an edge as zeros.  The steps are the edges' query heads: `share`
 // for each edge, U of them in flight.
 template <typename T, int V>
 __global__ __launch_bounds__(AT) void k_attend_grad_keys(Attend a, IdSort so, T *dk, T *dv, int vph,
-                                                         int64_t sum_blocks) {
+                                                         int64_t zero_blocks) {
   constexpr int U = 2;
   extern __shared__ int2 s_entries[];
   const int lg = so.lg, sub = threadIdx.x & ((1 << lg) - 1), g = threadIdx.x >> lg;
@@ -772,17 +772,15 @@ __global__ __launch_bounds__(AT) void k_attend_grad_keys(Attend a, IdSort so, T 
   const int kvh = min(at / vph, a.kv_heads - 1);
   const Piece<V> pc(at < a.kv_heads * vph ? at - kvh * vph : vph, a.D);
   const int64_t width = (int64_t)a.kv_heads * a.D;
-  if ((int64_t)blockIdx.x >= sum_blocks) {
-    const int64_t groups = ((int64_t)gridDim.x - sum_blocks) * per;
+  if ((int64_t)blockIdx.x < zero_blocks) {
     const float zero[V] = {};
-    for (int64_t r = ((int64_t)blockIdx.x - sum_blocks) * per + g; r < a.nkv; r += groups) {
-      if (so.seen[r]) continue;
+    absent_rows(so, lg, (int64_t)blockIdx.x * per + g, zero_blocks * per, [&](int64_t r) {
       st_piece<false>(from_floats<T, V>(zero), dk + r * width + kvh * a.D, pc);
       st_piece<false>(from_floats<T, V>(zero), dv + r * width + kvh * a.D, pc);
-    }
+    });
     return;
   }
-  const int64_t c = (int64_t)blockIdx.x * per + g;
+  const int64_t c = ((int64_t)blockIdx.x - zero_blocks) * per + g;
   if (c >= so.chunks) return;
   const uint32_t limit = (uint32_t)a.nkv;
   const float2 *pd = a.pd + kvh * a.share;
@@ -1252,12 +1250,11 @@ extern "C" int dg_attend_edges_grad(
       launch_join<T, true>(a, stream);
       const int per = AT >> lanes.lg;
       const int64_t sums = (so.chunks + per - 1) / per;
-      int64_t zeros = (nkv + 8 * per - 1) / (8 * per);
-      if (zeros > 4096) zeros = 4096;
+      const int64_t zeros = absent_blocks(so);
       hipLaunchKernelGGL((k_attend_grad_keys<T, V>),
                          dim3((unsigned)(sums + zeros), (unsigned)lanes.tiles), dim3(AT),
                          walk_bytes(so, lanes.lg), stream, a, so, static_cast<T *>(grad_k),
-                         static_cast<T *>(grad_v), vph, sums);
+                         static_cast<T *>(grad_v), vph, zeros);
       return (int)DG_OK;
     });
     if (grad_bias && !a.db) {

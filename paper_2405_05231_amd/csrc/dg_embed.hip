@@ -97,24 +97,24 @@ int launch_rows(const void *table, int64_t N, int cols, int64_t stride, const fl
 
 // ------------------------------------------------------------------ gradient
 // A group of 2^lg lanes adds the entries of one chunk of the sorted list, a vector
-// of columns each (dg_segments.h); blocks from sum_blocks on write the rows of nodes
-// that do not occur as zeros (a gradient in full).
+// of columns each (dg_segments.h); the first zero_blocks write the rows of nodes that do
+// not occur as zeros (a gradient in full).
 template <typename T, typename TO, int V>
 __global__ __launch_bounds__(ET) void k_embed_sum(IdSort a, uint32_t limit, const T *src,
                                                   int64_t stride, int cols, float scale, TO *out,
-                                                  int64_t out_stride, int64_t sum_blocks) {
+                                                  int64_t out_stride, int64_t zero_blocks) {
   extern __shared__ int2 s_entries[];
   const int lg = a.lg, sub = threadIdx.x & ((1 << lg) - 1), g = threadIdx.x >> lg;
   const Piece<V> pc((blockIdx.y << lg) + sub, cols);
   const int per = ET >> lg;
-  if ((int64_t)blockIdx.x >= sum_blocks) {
-    const int64_t groups = ((int64_t)gridDim.x - sum_blocks) * per;
+  if ((int64_t)blockIdx.x < zero_blocks) {
     const float zero[V] = {};
-    for (int64_t r = ((int64_t)blockIdx.x - sum_blocks) * per + g; r < a.slots; r += groups)
-      if (!a.seen[r]) st_piece<false>(from_floats<TO, V>(zero), out + r * out_stride, pc);
+    absent_rows(a, lg, (int64_t)blockIdx.x * per + g, zero_blocks * per, [&](int64_t r) {
+      st_piece<false>(from_floats<TO, V>(zero), out + r * out_stride, pc);
+    });
     return;
   }
-  const int64_t c = (int64_t)blockIdx.x * per + g;
+  const int64_t c = ((int64_t)blockIdx.x - zero_blocks) * per + g;
   if (c >= a.chunks) return;
   src += pc.at;
   float acc[V] = {};
@@ -221,13 +221,6 @@ __global__ __launch_bounds__(KT) void k_join(IdSort a, JoinOut o, int cols, int 
     }
     __syncthreads();
   }
-}
-
-// Zero blocks: about eight rows for each group of lanes, at most 4096 blocks.
-int64_t zero_blocks(const IdSort &a, int lg) {
-  if (a.compact) return 0;
-  const int64_t b = (a.slots + 8 * (ET >> lg) - 1) / (8 * (ET >> lg));
-  return b > 4096 ? 4096 : b;
 }
 
 // The sort of a list for sums of rows of D elements by groups of 2^lg lanes.
@@ -346,11 +339,11 @@ extern "C" int dg_embed_rows_grad(const void *grad_out, int32_t type, int64_t gr
       return with_vec<T>(D, [&](auto v) {
         constexpr int V = decltype(v)::value;
         const int per = ET >> a.lg;
-        const int64_t sums = (a.chunks + per - 1) / per;
+        const int64_t sums = (a.chunks + per - 1) / per, zeros = absent_blocks(a);
         hipLaunchKernelGGL((k_embed_sum<T, TO, V>),
-                           dim3((unsigned)(sums + zero_blocks(a, a.lg)), (unsigned)lanes.tiles),
+                           dim3((unsigned)(sums + zeros), (unsigned)lanes.tiles),
                            dim3(ET), walk_bytes(a, a.lg), stream, a, a.limit(),
-                           (const T *)grad_out, grad_stride, (int)D, scale, (TO *)grad, D, sums);
+                           (const T *)grad_out, grad_stride, (int)D, scale, (TO *)grad, D, zeros);
         DG_HIP(hipGetLastError());
         const JoinOut j = {{grad, nullptr}, {D, 0}, {0, 0}, {scale, 0.f}};
         return run_join(a, j, 1, (int)D, grad_type, stream);

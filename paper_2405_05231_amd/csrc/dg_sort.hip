@@ -69,10 +69,7 @@ __global__ __launch_bounds__(ST) void k_sort_count(IdSort a, Pass p, int32_t *st
 #pragma unroll
     for (int r = 0; r < COUNT_FLIGHT; ++r) {
       if (t0 + r0 + r * 64 + lane >= a.n) continue;
-      if (FIRST) {
-        k[r] = sort_key(k[r], a.slots, &bad);
-        if (!a.compact && k[r] < a.slots) a.seen[k[r]] = 1;
-      }
+      if (FIRST) k[r] = sort_key(k[r], a.slots, &bad);
       atomicAdd(&s_cnt[w][((uint32_t)k[r] >> p.shift) & (bins - 1)], 1u);
     }
   }
@@ -250,8 +247,6 @@ __global__ __launch_bounds__(ST) void k_heads_rank(IdSort a, const int32_t *key,
 // ------------------------------------------------------------------ short lists
 // One block, 8 bits a pass: a wave holds 128 entries in a row, ranks them as
 // k_sort_place does, and the passes exchange them through shared memory.
-// tables whose marks that block clears by itself, which is worth a launch
-constexpr int64_t SMALL_SEEN = 1 << 17;
 constexpr int SMALL_T = 1024, SMALL_W = SMALL_T / 64, SMALL_BITS = 8;
 __global__ __launch_bounds__(SMALL_T) void k_sort_small(IdSort a, int32_t *node_out,
                                                         int64_t *count, int32_t *status) {
@@ -263,16 +258,10 @@ __global__ __launch_bounds__(SMALL_T) void k_sort_small(IdSort a, int32_t *node_
   const uint64_t lt = lanes_below();
   int2 x[R];
   bool bad = false;
-  if (!a.compact && a.slots <= SMALL_SEEN) {  // else run_sort has cleared them
-    for (int64_t i = threadIdx.x; i < (a.slots + 15) / 16; i += SMALL_T)
-      reinterpret_cast<uint4 *>(a.seen)[i] = uint4{0, 0, 0, 0};
-    __syncthreads();
-  }
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int i = w * (64 * R) + r * 64 + lane;
     x[r] = int2{i < n ? sort_key(a.ids[i], a.slots, &bad) : 0, i};
-    if (!a.compact && i < n && x[r].x < a.slots) a.seen[x[r].x] = 1;
   }
   if (bad && status) atomicOr(status, 1);
   if (threadIdx.x == 0) *a.n_long = 0;
@@ -379,7 +368,6 @@ void carve_sort(IdSort &a, Carve &c) {
   a.dst = a.key[0];
   a.order = a.pos[0];
   if (a.compact) a.dst = c.take<int32_t>((size_t)n);
-  a.seen = a.compact ? nullptr : c.take<uint8_t>((size_t)a.slots);
   a.cnt = c.take<uint32_t>((size_t)BINS * (size_t)tiles);
   a.tot = c.take<uint32_t>(BINS);
   a.heads = a.compact ? c.take<int32_t>((size_t)((n + HEADS - 1) / HEADS)) : nullptr;
@@ -402,10 +390,6 @@ size_t sort_room(IdSort a) {
 }
 
 int run_sort(IdSort &a, int32_t *node_out, int64_t *count, int32_t *status, hipStream_t s) {
-  if (!a.compact && (a.n == 0 || a.n > SMALL || a.slots > SMALL_SEEN)) {
-    // (carved in pieces of 256 bytes, so whole words hold it)
-    DG_TRY(fill_u64((uint64_t *)a.seen, (size_t)(a.slots + 7) / 8, 0, s));
-  }
   if (a.n == 0) return a.compact ? fill_u64((uint64_t *)count, 1, 0, s) : DG_OK;
   if (a.n <= SMALL) {
     hipLaunchKernelGGL(k_sort_small, dim3(1), dim3(SMALL_T), 0, s, a, node_out, count, status);
