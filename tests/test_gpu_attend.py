@@ -544,3 +544,45 @@ def test_long_lists_with_every_head_layout(dg, dtype, heads, kv_heads, D):
     query heads of a key head."""
     p = problem([2, 700, 0, 5, 131, 1], 90, heads, kv_heads, D, dtype, "edge")
     check_gradient(dg, p, check_forward(dg, p))
+
+
+@pytest.mark.parametrize("lens", [[3, 5, 300, 2], [4] * 300, [0, 600, 1, 700, 0, 9]])
+def test_bad_offsets_touch_nothing_else(dg, lens):
+    """Offsets out of order or range in every place: reported, rows elsewhere in the list keep
+    their results or are left out, and nothing is written beside outputs and workspace."""
+    p = problem(lens, 20, 2, 2, 8, torch.float32, "edge")
+    nq, E = len(lens), p["indices"].numel()
+    q, k, v = p["q"], p["k"], p["v"]
+    need = dg._L.dg_attend_edges_grad_workspace_bytes(E, 20, 2, 2, 8)
+    room = torch.full((need + 8192,), 0x5A, dtype=torch.uint8, device=DEV)
+    ws = room[4096:4096 + need]
+    assert ws.data_ptr() % 256 == 0
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    good = p["offsets"].clone()
+    for at in {0, 1, nq // 2, nq - 1, nq}:
+        for value in (-1, 2 ** 40, E + 1, E, 0, -2 ** 62):
+            off = good.clone()
+            if int(off[at]) == value:
+                continue
+            off[at] = value
+            status.zero_()
+            r = dg.attend_edges(q, k, v, off, p["indices"], bias=p["bias"], workspace=ws,
+                                status=status)
+            g = dg.attend_edges_grad(q, q, k, v, r.out, r.lse, off, p["indices"], bias=p["bias"],
+                                     workspace=ws)
+            torch.cuda.synchronize()
+            ordered = bool((off.diff() >= 0).all()) and value >= 0 and value <= E
+            assert ordered or int(status) & 2, (at, value)
+            assert (room[:4096] == 0x5A).all() and (room[4096 + need:] == 0x5A).all()
+            assert r.out.shape == g.q.shape
+
+
+@pytest.mark.parametrize("dtype", WIDE)
+@pytest.mark.parametrize("D", [1, 2, 4, 8])
+@pytest.mark.parametrize("lens", [[1, 0, 2] * 100, [1] * 64, [3, 1] * 33, [0] * 65, [2] * 5000])
+def test_narrow_heads_with_short_lists(dg, dtype, D, lens):
+    """One head of a vector or less and lists of a few edges: the most rows that a wave takes."""
+    p = problem(lens, 50, 1, 1, D, dtype)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    check_gradient(dg, p, check_forward(dg, p, status=status), status=status)
+    assert int(status) == 0
