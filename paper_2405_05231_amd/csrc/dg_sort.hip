@@ -4,8 +4,9 @@
 // wave come from ballots, so that equal IDs cost no atomics and keep their order.
 // Lists of up to SMALL entries are sorted by one block in shared memory.
 //
-// Bound by the launches below some 10^5 entries and by the scattered 8-byte writes of
-// the place pass above.
+// Bound by the launches below some 10^5 entries and by the scattered writes of the place
+// pass above: 1.2M IDs of 25 bits take three passes of 6 + 4 + 16 us, 600,001 of 18 bits
+// two of 6 + 5 + 11, 1500 in one block 6.6 us.
 #include "dg_segments.h"
 
 namespace dg {
