@@ -851,17 +851,14 @@ __global__ __launch_bounds__(AT) void k_attend_grad_bias(Attend a, float *db) {
   }
 }
 
-// Rows without keys at all.
-template <typename T>
-__global__ __launch_bounds__(AT) void k_fill_rows(T *p, int64_t n, float value) {
+// lse of rows without keys at all.
+__global__ __launch_bounds__(AT) void k_fill_rows(float *p, int64_t n, float value) {
   for (int64_t i = (int64_t)blockIdx.x * AT + threadIdx.x; i < n; i += (int64_t)gridDim.x * AT)
-    p[i] = (T)value;
+    p[i] = value;
 }
-template <typename T>
-void fill_rows(T *p, int64_t n, float value, hipStream_t s) {
-  if (n < 1) return;
+void fill_rows(float *p, int64_t n, float value, hipStream_t s) {
   const int64_t b = (n + AT - 1) / AT;
-  hipLaunchKernelGGL(k_fill_rows<T>, dim3((unsigned)(b > 4096 ? 4096 : b)), dim3(AT), 0, s, p, n,
+  hipLaunchKernelGGL(k_fill_rows, dim3((unsigned)(b > 4096 ? 4096 : b)), dim3(AT), 0, s, p, n,
                      value);
 }
 
@@ -1096,7 +1093,7 @@ extern "C" int dg_attend_edges(const void *q, int64_t q_stride, const void *k, i
   return with_type(type, [&](auto t) {
     using T = decltype(t);
     if (num_edges == 0) {
-      fill_rows(static_cast<T *>(out), nq * qw, 0.f, stream);
+      DG_TRY(run_clear(out, nq * qw * b, stream));
       fill_rows(lse, nq * heads, NINF, stream);
       DG_HIP(hipGetLastError());
       return (int)DG_OK;
@@ -1201,10 +1198,9 @@ extern "C" int dg_attend_edges_grad(
   return with_type(type, [&](auto t) {
     using T = decltype(t);
     if (num_edges == 0) {
-      fill_rows(static_cast<T *>(grad_q), nq * qw, 0.f, stream);
-      fill_rows(static_cast<T *>(grad_k), nkv * kw, 0.f, stream);
-      fill_rows(static_cast<T *>(grad_v), nkv * kw, 0.f, stream);
-      DG_HIP(hipGetLastError());
+      if (nq) DG_TRY(run_clear(grad_q, nq * qw * b, stream));
+      if (nkv) DG_TRY(run_clear(grad_k, nkv * kw * b, stream));
+      if (nkv) DG_TRY(run_clear(grad_v, nkv * kw * b, stream));
       return (int)DG_OK;
     }
     Attend a;
@@ -1246,6 +1242,11 @@ extern "C" int dg_attend_edges_grad(
     carve_sort(so, c);
     so.place = r.place;
     DG_TRY(run_sort(so, nullptr, nullptr, status, stream));
+    const bool cleared = clear_first(so, 2 * nkv * kw * b);
+    if (cleared) {
+      DG_TRY(run_clear(grad_k, nkv * kw * b, stream));
+      DG_TRY(run_clear(grad_v, nkv * kw * b, stream));
+    }
     bool all_heads = false;
     (void)with_vec<T>(D, [&](auto v) {
       constexpr int V = decltype(v)::value;
@@ -1262,7 +1263,7 @@ extern "C" int dg_attend_edges_grad(
       launch_join<T, true>(a, stream);
       const int per = AT >> lanes.lg;
       const int64_t sums = (so.chunks + per - 1) / per;
-      const int64_t zeros = absent_blocks(so);
+      const int64_t zeros = absent_blocks(so, cleared);
       hipLaunchKernelGGL((k_attend_grad_keys<T, V>),
                          dim3((unsigned)(sums + zeros), (unsigned)lanes.tiles), dim3(AT),
                          walk_bytes(so, lanes.lg), stream, a, so, static_cast<T *>(grad_k),

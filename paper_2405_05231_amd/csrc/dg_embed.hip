@@ -239,7 +239,29 @@ void set_sort(IdSort &a, const int32_t *ids, int64_t n, int64_t N, int64_t D, bo
   a.width = D;
 }
 
+// A thread stores CU vectors of 16 bytes, a block's span of them one after the other; the
+// last thread adds the bytes that fill no vector.
+constexpr int CU = 4;
+__global__ __launch_bounds__(ET) void k_clear(char *p, int64_t bytes) {
+  typedef u32x4 u32x4_any __attribute__((aligned(1)));
+  const int64_t vecs = bytes / 16;
+#pragma unroll
+  for (int u = 0; u < CU; ++u) {
+    const int64_t i = ((int64_t)blockIdx.x * CU + u) * ET + threadIdx.x;
+    if (i < vecs) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4_any *>(p) + i);
+    if (i == vecs)
+      for (int64_t b = vecs * 16; b < bytes; ++b) p[b] = 0;
+  }
+}
+
 }  // namespace
+
+int run_clear(void *p, int64_t bytes, hipStream_t s) {
+  const int64_t blocks = (bytes / 16 + ET * CU) / (ET * CU);
+  hipLaunchKernelGGL(k_clear, dim3((unsigned)blocks), dim3(ET), 0, s, static_cast<char *>(p), bytes);
+  DG_HIP(hipGetLastError());
+  return DG_OK;
+}
 
 int run_join(const IdSort &a, const JoinOut &o, int outs, int cols, int32_t type, hipStream_t s) {
   if (!a.part) return DG_OK;  // too short a list for a long segment
@@ -335,7 +357,9 @@ extern "C" int dg_embed_rows_grad(const void *grad_out, int32_t type, int64_t gr
   Carve c(ws);
   carve_sort(a, c);
   DG_TRY(run_sort(a, rows, num_rows, status, stream));
-  if (n == 0 && sparse) return DG_OK;
+  const bool cleared = clear_first(a, out_bytes);
+  if (cleared) DG_TRY(run_clear(grad, out_bytes, stream));
+  if (n == 0 && (sparse || cleared)) return DG_OK;
   return with_type(type, [&](auto in) {
     return with_type(grad_type, [&](auto o) {
       using T = decltype(in);
@@ -343,7 +367,7 @@ extern "C" int dg_embed_rows_grad(const void *grad_out, int32_t type, int64_t gr
       return with_vec<T>(D, [&](auto v) {
         constexpr int V = decltype(v)::value;
         const int per = ET >> a.lg;
-        const int64_t sums = (a.chunks + per - 1) / per, zeros = absent_blocks(a);
+        const int64_t sums = (a.chunks + per - 1) / per, zeros = absent_blocks(a, cleared);
         hipLaunchKernelGGL((k_embed_sum<T, TO, V>),
                            dim3((unsigned)(sums + zeros), (unsigned)lanes.tiles),
                            dim3(ET), walk_bytes(a, a.lg), stream, a, a.limit(),

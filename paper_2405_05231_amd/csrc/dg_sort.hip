@@ -16,7 +16,7 @@ constexpr int ST = 256;            // threads of a tile's block
 constexpr int SW = ST / 64;
 constexpr int MAX_BITS = 10;       // of a digit
 constexpr int BINS = 1 << MAX_BITS;
-constexpr int SMALL = 2048;
+constexpr int SMALL = 8192;
 constexpr int HEADS = 1024;        // entries of a block of k_heads_*
 constexpr int COUNT_FLIGHT = 16;   // entries per lane whose keys are loaded together
 
@@ -246,14 +246,15 @@ __global__ __launch_bounds__(ST) void k_heads_rank(IdSort a, const int32_t *key,
 }
 
 // ------------------------------------------------------------------ short lists
-// One block, 8 bits a pass: a wave holds 128 entries in a row, ranks them as
+// One block, 8 bits a pass: a wave holds 64 R entries in a row, ranks them as
 // k_sort_place does, and the passes exchange them through shared memory.
 constexpr int SMALL_T = 1024, SMALL_W = SMALL_T / 64, SMALL_BITS = 8;
+template <int R>
 __global__ __launch_bounds__(SMALL_T) void k_sort_small(IdSort a, int32_t *node_out,
                                                         int64_t *count, int32_t *status) {
-  constexpr int R = SMALL / SMALL_T, SB = 1 << SMALL_BITS;
+  constexpr int SB = 1 << SMALL_BITS;
   __shared__ uint32_t s_at[SMALL_W][SB];
-  __shared__ int2 s[SMALL];
+  __shared__ int2 s[R * SMALL_T];
   __shared__ int32_t s_sum[SB / 64];
   const int n = (int)a.n, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const uint64_t lt = lanes_below();
@@ -393,7 +394,13 @@ size_t sort_room(IdSort a) {
 int run_sort(IdSort &a, int32_t *node_out, int64_t *count, int32_t *status, hipStream_t s) {
   if (a.n == 0) return a.compact ? fill_u64((uint64_t *)count, 1, 0, s) : DG_OK;
   if (a.n <= SMALL) {
-    hipLaunchKernelGGL(k_sort_small, dim3(1), dim3(SMALL_T), 0, s, a, node_out, count, status);
+    const dim3 one(1), t(SMALL_T);
+    if (a.n <= 2 * SMALL_T)
+      hipLaunchKernelGGL(k_sort_small<2>, one, t, 0, s, a, node_out, count, status);
+    else if (a.n <= 4 * SMALL_T)
+      hipLaunchKernelGGL(k_sort_small<4>, one, t, 0, s, a, node_out, count, status);
+    else
+      hipLaunchKernelGGL(k_sort_small<8>, one, t, 0, s, a, node_out, count, status);
     DG_HIP(hipGetLastError());
     return DG_OK;
   }

@@ -284,3 +284,27 @@ def test_refusals(dg):
         dg.embed_rows_grad(randn(1, 4, 8), ids, 10, out=randn(1, 9, 8))
     with pytest.raises(dg.DGError):
         dg.embed_rows_grad(randn(1, 4, 8), ids, 0)
+
+
+@pytest.mark.parametrize("n", [4095, 4096, 4097, 8191, 8192, 8193, 12000])
+@pytest.mark.parametrize("N", [1, 300, 70_000, 20_000_000])
+def test_gradient_lists_around_one_blocks_reach(dg, n, N):
+    ids = torch.randint(-1, N, (n,), device=DEV, dtype=torch.int32, generator=rng(n))
+    ids[::3] = ids[0].clamp(min=0)  # a long segment
+    run_both(dg, randn(1, n, 20), ids, N)
+
+
+@pytest.mark.parametrize("dtype,N,D", [(torch.float32, 700_001, 129), (torch.bfloat16, 900_001, 201)])
+@pytest.mark.parametrize("n", [0, 1, 5000, 340_000, 360_000])
+def test_gradient_of_large_tables_with_few_entries(dg, dtype, N, D, n):
+    """On both sides of the share of rows from which a large result is cleared first, into a
+    buffer of garbage with odd bytes at its end."""
+    ids = torch.randint(0, N, (n,), device=DEV, dtype=torch.int32, generator=rng(5))
+    g = randn(1, n, D, dtype=dtype)
+    room = torch.full((N * D + 9,), 7.0, dtype=dtype, device=DEV)
+    out = room[3:3 + N * D].view(N, D)
+    dg.embed_rows_grad(g, ids, N, out=out)
+    nodes, sums, mags, counts = plain_grad(g, ids, N, 1.0)
+    check_grad(out[nodes.long()], sums, mags, counts, dtype)
+    out[nodes.long()] = 0
+    assert not out.any() and (room[:3] == 7).all() and (room[3 + N * D:] == 7).all()
