@@ -239,25 +239,20 @@ void set_sort(IdSort &a, const int32_t *ids, int64_t n, int64_t N, int64_t D, bo
   a.width = D;
 }
 
-// A thread stores CU vectors of 16 bytes, a block's span of them one after the other; the
-// last thread adds the bytes that fill no vector.
-constexpr int CU = 4;
+// A vector of 16 bytes a thread; the one behind the last whole vector stores the bytes that
+// fill none.  (407 MB: 61 us, 6.7 TB/s; four vectors a thread 72, with nontemporal stores 73.)
 __global__ __launch_bounds__(ET) void k_clear(char *p, int64_t bytes) {
   typedef u32x4 u32x4_any __attribute__((aligned(1)));
-  const int64_t vecs = bytes / 16;
-#pragma unroll
-  for (int u = 0; u < CU; ++u) {
-    const int64_t i = ((int64_t)blockIdx.x * CU + u) * ET + threadIdx.x;
-    if (i < vecs) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, reinterpret_cast<u32x4_any *>(p) + i);
-    if (i == vecs)
-      for (int64_t b = vecs * 16; b < bytes; ++b) p[b] = 0;
-  }
+  const int64_t vecs = bytes / 16, i = (int64_t)blockIdx.x * ET + threadIdx.x;
+  if (i < vecs) *(reinterpret_cast<u32x4_any *>(p) + i) = u32x4{0, 0, 0, 0};
+  if (i == vecs)
+    for (int64_t b = vecs * 16; b < bytes; ++b) p[b] = 0;
 }
 
 }  // namespace
 
 int run_clear(void *p, int64_t bytes, hipStream_t s) {
-  const int64_t blocks = (bytes / 16 + ET * CU) / (ET * CU);
+  const int64_t blocks = bytes / 16 / ET + 1;
   hipLaunchKernelGGL(k_clear, dim3((unsigned)blocks), dim3(ET), 0, s, static_cast<char *>(p), bytes);
   DG_HIP(hipGetLastError());
   return DG_OK;
