@@ -1241,12 +1241,13 @@ extern "C" int dg_attend_edges_grad(
     set_edge_sort(so, indices, num_edges, nkv, kv_heads, D, lanes.lg);
     carve_sort(so, c);
     so.place = r.place;
-    DG_TRY(run_sort(so, nullptr, nullptr, status, stream));
     const bool cleared = clear_first(so, 2 * nkv * kw * b);
     if (cleared) {
-      DG_TRY(run_clear(grad_k, nkv * kw * b, stream));
-      DG_TRY(run_clear(grad_v, nkv * kw * b, stream));
+      so.clear[0] = static_cast<char *>(grad_k);
+      so.clear[1] = static_cast<char *>(grad_v);
+      so.clear_bytes = nkv * kw * b;
     }
+    DG_TRY(run_sort(so, nullptr, nullptr, status, stream));
     bool all_heads = false;
     (void)with_vec<T>(D, [&](auto v) {
       constexpr int V = decltype(v)::value;

@@ -239,14 +239,10 @@ void set_sort(IdSort &a, const int32_t *ids, int64_t n, int64_t N, int64_t D, bo
   a.width = D;
 }
 
-// A vector of 16 bytes a thread; the one behind the last whole vector stores the bytes that
-// fill none.  (407 MB: 61 us, 6.7 TB/s; four vectors a thread 72, with nontemporal stores 73.)
+// A vector a thread (407 MB: 61 us, 6.7 TB/s; four vectors a thread 72, with nontemporal
+// stores 73).
 __global__ __launch_bounds__(ET) void k_clear(char *p, int64_t bytes) {
-  typedef u32x4 u32x4_any __attribute__((aligned(1)));
-  const int64_t vecs = bytes / 16, i = (int64_t)blockIdx.x * ET + threadIdx.x;
-  if (i < vecs) *(reinterpret_cast<u32x4_any *>(p) + i) = u32x4{0, 0, 0, 0};
-  if (i == vecs)
-    for (int64_t b = vecs * 16; b < bytes; ++b) p[b] = 0;
+  clear_vector(p, bytes, (int64_t)blockIdx.x * ET + threadIdx.x);
 }
 
 }  // namespace
@@ -351,9 +347,12 @@ extern "C" int dg_embed_rows_grad(const void *grad_out, int32_t type, int64_t gr
     return set_error(DG_EWORKSPACE, "dg_embed_rows_grad: workspace needs %zu bytes", size.used);
   Carve c(ws);
   carve_sort(a, c);
-  DG_TRY(run_sort(a, rows, num_rows, status, stream));
   const bool cleared = clear_first(a, out_bytes);
-  if (cleared) DG_TRY(run_clear(grad, out_bytes, stream));
+  if (cleared) {
+    a.clear[0] = static_cast<char *>(grad);
+    a.clear_bytes = out_bytes;
+  }
+  DG_TRY(run_sort(a, rows, num_rows, status, stream));
   if (n == 0 && (sparse || cleared)) return DG_OK;
   return with_type(type, [&](auto in) {
     return with_type(grad_type, [&](auto o) {

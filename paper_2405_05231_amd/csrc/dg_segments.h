@@ -25,6 +25,8 @@ struct IdSort {
   int64_t n, slots;
   bool compact;        // dst = rank among the distinct nodes, not the node
   int lg;              // lanes that take a chunk: 2^lg
+  char *clear[2];      // results that run_sort clears (clear_first), of clear_bytes each
+  int64_t clear_bytes; // 0: none
   // carved
   int32_t *key[2], *pos[2];  // keys and list places, alternating between passes
   int32_t *dst;        // [n] row that each sorted entry is added to: below limit(), or
@@ -142,6 +144,15 @@ inline bool clear_first(const IdSort &a, int64_t bytes) {
 }
 // Zeroes `bytes` bytes at any alignment.
 int run_clear(void *p, int64_t bytes, hipStream_t s);
+// A vector of 16 bytes, vector i of them; the one behind the last whole vector stores the
+// bytes that fill none.
+__device__ __forceinline__ void clear_vector(char *p, int64_t bytes, int64_t i) {
+  typedef u32x4 u32x4_any __attribute__((aligned(1)));
+  const int64_t vecs = bytes / 16;
+  if (i < vecs) *(reinterpret_cast<u32x4_any *>(p) + i) = u32x4{0, 0, 0, 0};
+  if (i == vecs)
+    for (int64_t b = vecs * 16; b < bytes; ++b) p[b] = 0;
+}
 
 // Calls zero(row) for the nodes in [0, slots) that do not occur, 2^lg of them to a group of
 // lanes at a time: each lane looks one up in the sorted list.  (Marks of the nodes that

@@ -253,6 +253,11 @@ template <int R>
 __global__ __launch_bounds__(SMALL_T) void k_sort_small(IdSort a, int32_t *node_out,
                                                         int64_t *count, int32_t *status) {
   constexpr int SB = 1 << SMALL_BITS;
+  if (blockIdx.x) {  // the other blocks clear results meanwhile
+    const int64_t each = (a.clear_bytes / 16 / SMALL_T) + 1, b = (int64_t)blockIdx.x - 1;
+    clear_vector(a.clear[b >= each], a.clear_bytes, (b % each) * SMALL_T + threadIdx.x);
+    return;
+  }
   __shared__ uint32_t s_at[SMALL_W][SB];
   __shared__ int2 s[R * SMALL_T];
   __shared__ int32_t s_sum[SB / 64];
@@ -392,9 +397,14 @@ size_t sort_room(IdSort a) {
 }
 
 int run_sort(IdSort &a, int32_t *node_out, int64_t *count, int32_t *status, hipStream_t s) {
+  if (a.clear_bytes && (a.n == 0 || a.n > SMALL)) {
+    for (char *p : a.clear)
+      if (p) DG_TRY(run_clear(p, a.clear_bytes, s));
+  }
   if (a.n == 0) return a.compact ? fill_u64((uint64_t *)count, 1, 0, s) : DG_OK;
   if (a.n <= SMALL) {
-    const dim3 one(1), t(SMALL_T);
+    const int64_t each = a.clear_bytes ? a.clear_bytes / 16 / SMALL_T + 1 : 0;
+    const dim3 one((unsigned)(1 + (a.clear[1] ? 2 : 1) * each)), t(SMALL_T);
     if (a.n <= 2 * SMALL_T)
       hipLaunchKernelGGL(k_sort_small<2>, one, t, 0, s, a, node_out, count, status);
     else if (a.n <= 4 * SMALL_T)

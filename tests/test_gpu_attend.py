@@ -586,3 +586,25 @@ def test_narrow_heads_with_short_lists(dg, dtype, D, lens):
     status = torch.zeros(1, dtype=torch.int32, device=DEV)
     check_gradient(dg, p, check_forward(dg, p, status=status), status=status)
     assert int(status) == 0
+
+
+@pytest.mark.parametrize("E", [0, 3000, 30_000])
+def test_few_edges_into_many_keys(dg, E):
+    """Gradients so large and so empty that they are cleared as a whole first: the same bits as
+    among the keys that occur alone, zeros elsewhere."""
+    nkv, heads, D = 1_300_001, 2, 33
+    p = problem([5] * (E // 5) if E else [0], nkv, heads, heads, D, torch.float32)
+    k, v = p["k"], p["v"]
+    idx = p["indices"]
+    used, at = idx.unique(return_inverse=True)
+    r = dg.attend_edges(p["q"], k, v, p["offsets"], idx)
+    junk = torch.full((2 * nkv, heads, D), 7.0, device=DEV)  # what the allocator may hand out
+    del junk
+    g = dg.attend_edges_grad(p["q"], p["q"], k, v, r.out, r.lse, p["offsets"], idx)
+    u = used.long()
+    small = dg.attend_edges_grad(p["q"], p["q"], k[u], v[u], r.out, r.lse, p["offsets"], at.int())
+    assert torch.equal(g.k[u], small.k) and torch.equal(g.v[u], small.v)
+    assert torch.equal(g.q, small.q)
+    g.k[u] = 0
+    g.v[u] = 0
+    assert not g.k.any() and not g.v.any()
