@@ -451,12 +451,12 @@ __device__ __forceinline__ void take_work(const Attend &a, Stage *s, Task task) 
     if (r0 >= a.nq) return;
     tasks = (int)min((int64_t)(slots * a.rounds), a.nq - r0);  // rows: at most 32
     off = a.offsets[r0 + min(lane, tasks)];
-    // the wave's lists are one run of edges; where its ends are out of order, its lists are
-    // read from where they stand
+    // the wave's lists are one run of edges; where its ends are out of order or range, all
+    // of them are left out
     const int64_t e0 = read_lane(off, 0), e1 = read_lane(off, tasks);
     const bool run = list_ok(a, e0, e1);
-    g = run ? stage<GRAD>(a, s, e0, e1) : Staged{s, 0, false};
-    stop = run ? e1 : a.edges;
+    stop = run ? e1 : 0;
+    g = stage<GRAD>(a, s, run ? e0 : 0, stop);
   } else {
     if (unit >= a.chunks) return;
     const int64_t lo = unit * a.ch, hi = min(lo + a.ch, a.edges);
@@ -489,7 +489,7 @@ __device__ __forceinline__ void take_work(const Attend &a, Stage *s, Task task) 
     int64_t row, slot = -2;
     if (by_rows) {
       const bool there = at < tasks;
-      const bool ok = list_ok(a, start, end) && start >= g.e0 && end <= stop;
+      const bool ok = g.e0 <= start && start <= end && end <= stop;
       if (there && !ok && a.status) atomicOr(a.status, 2);
       if (!ok) end = start;
       if (there && !(a.chunks && end - start > a.ch)) slot = -1;
