@@ -443,20 +443,21 @@ __device__ __forceinline__ void take_work(const Attend &a, Stage *s, Task task) 
   const int slots = 64 >> (LaneT::lg_g(a) + a.lg_h + lg_e);  // 1 for chunks
   const int64_t unit =
       ((int64_t)blockIdx.x - (by_rows ? a.chunk_blocks : 0)) * AW + wave;  // wave or chunk
-  int64_t r0 = 0, off, first = -1, last = -1, stop = 0;
-  int tasks;
+  int64_t r0 = 0, first = -1, last = -1;
+  int tasks, rel;  // rel: a lane's offset counted from g.e0, -1 outside the run
+
   Staged g;
   if (by_rows) {
     r0 = unit * slots * a.rounds;
     if (r0 >= a.nq) return;
     tasks = (int)min((int64_t)(slots * a.rounds), a.nq - r0);  // rows: at most 32
-    off = a.offsets[r0 + min(lane, tasks)];
+    const int64_t off = a.offsets[r0 + min(lane, tasks)];
     // the wave's lists are one run of edges; where its ends are out of order or range, all
     // of them are left out
     const int64_t e0 = read_lane(off, 0), e1 = read_lane(off, tasks);
     const bool run = list_ok(a, e0, e1);
-    stop = run ? e1 : 0;
-    g = stage<GRAD>(a, s, run ? e0 : 0, stop);
+    rel = run && off >= e0 && off <= e1 ? (int)(off - e0) : -1;
+    g = stage<GRAD>(a, s, run ? e0 : 0, run ? e1 : 0);
   } else {
     if (unit >= a.chunks) return;
     const int64_t lo = unit * a.ch, hi = min(lo + a.ch, a.edges);
@@ -475,21 +476,19 @@ __device__ __forceinline__ void take_work(const Attend &a, Stage *s, Task task) 
       a.starts[unit] = begin ? mine : -1;
     if (!cuts) return;
     tasks = 2;
-    off = cut ? max(start, lo) : lo;  // lane 0 to 3: starts and ends
-    const int64_t ends = __shfl(cut ? min(end, hi) : lo, lane & 1, 64);
-    off = lane < 2 ? off : ends;
+    // lanes 0 and 1: where the two lists start in the chunk, 2 and 3: where they end
+    const int ends = __shfl(cut ? (int)(min(end, hi) - lo) : 0, lane & 1, 64);
+    rel = lane >= 2 ? ends : cut ? (int)(max(start, lo) - lo) : 0;
     g = stage<GRAD>(a, s, lo, hi);
   }
   const LaneT ln(a, lg_e);
 #pragma unroll 1
   for (int i = 0; i * slots < tasks; ++i) {
     const int at = i * slots + ln.rs;
-    int64_t start = __shfl(off, at & 63, 64);
-    int64_t end = __shfl(off, (by_rows ? at + 1 : at + 2) & 63, 64);
+    int start = __shfl(rel, at & 63, 64), end = __shfl(rel, (by_rows ? at + 1 : at + 2) & 63, 64);
     int64_t row, slot = -2;
     if (by_rows) {
-      const bool there = at < tasks;
-      const bool ok = g.e0 <= start && start <= end && end <= stop;
+      const bool there = at < tasks, ok = start >= 0 && end >= start;
       if (there && !ok && a.status) atomicOr(a.status, 2);
       if (!ok) end = start;
       if (there && !(a.chunks && end - start > a.ch)) slot = -1;
@@ -499,8 +498,8 @@ __device__ __forceinline__ void take_work(const Attend &a, Stage *s, Task task) 
       row = i ? last : first;
       slot = 2 * unit + i;
     }
-    if (slot == -2 || start >= end) start = end = g.e0;
-    task(ln, row, (int)(start - g.e0), (int)(end - g.e0), g, lg_e, slot);
+    if (slot == -2 || start >= end) start = end = 0;
+    task(ln, row, start, end, g, lg_e, slot);
   }
 }
 
